@@ -216,9 +216,9 @@ def prepare(case, seed):
                           torch.randint(0, most, (T,), generator=g, device=dev, dtype=torch.int32))
     if own:
         from paper_2603_09229_amd import binding as fk
-        s["cache"] = fk.KV4Cache(s["k_codes"], s["v_codes"], s["k_scale"], s["v_scale"], s["k_levels"], s["v_levels"])
+        s["cache"] = fk.KVCache(s["k_codes"], s["v_codes"], s["k_scale"], s["v_scale"], s["k_levels"], s["v_levels"])
         if case["kind"] == "attend":
-            s["ws"] = fk.make_kv4_workspace(s["cache"], case["B"], case["G"] * H, s["q"].shape[0], s["max_q"], s["max_len"])
+            s["ws"] = fk.make_kv_workspace(s["cache"], case["B"], case["G"] * H, s["q"].shape[0], s["max_q"], s["max_len"])
     return s
 
 
@@ -226,12 +226,12 @@ def _own(s):
     from paper_2603_09229_amd import binding as fk
     case = s["case"]
     if case["kind"] == "read":
-        return fk.fk_kv4_read(s["cache"], s["slots"])
+        return fk.fk_kv_read(s["cache"], s["slots"])
     if case["kind"] == "append":
-        q = fk.fk_kv4_append(s["cache"], s["k"], s["v"], s["slots"], positions=s["positions"], cos_sin=s["cos_sin"],
+        q = fk.fk_kv_append(s["cache"], s["k"], s["v"], s["slots"], positions=s["positions"], cos_sin=s["cos_sin"],
                              interleaved=case["interleaved"], q=s["q"])
-        return (q, *fk.fk_kv4_read(s["cache"], s["slots"]))
-    return fk.fk_kv4_attend(s["cache"], s["q"], s["pages"], s["lens"], q_start=s["q_start"], max_q=s["max_q"],
+        return (q, *fk.fk_kv_read(s["cache"], s["slots"]))
+    return fk.fk_kv_attend(s["cache"], s["q"], s["pages"], s["lens"], q_start=s["q_start"], max_q=s["max_q"],
                             max_len=s["max_len"], causal=True, window=case["window"], ws=s["ws"])
 
 
