@@ -285,6 +285,85 @@ int fk_set_option(const char* name, int value);
 void fk_stage_timer_start(void);
 int fk_stage_timer_stop(double* stage_ms, int* stage_launches);
 
+/*
+ * A paged key/value cache held in 4 bits.  The centroids of a fit with K = 16 clusters of single numbers are the
+ * 16 levels that 4-bit ids stand for: a key or value x of a row with largest magnitude s is kept as the id of
+ * the level nearest to x / s, and reads back as level * s.  Host struct of device pointers, owned by the caller:
+ *   k_codes, v_codes    [pages, heads, page_size, d/2] bytes; channel 2b in the low, 2b+1 in the high half of byte b
+ *   k_scale, v_scale    [pages, heads, page_size] of type t: the largest magnitude of the row (exact: rows are of type t);
+ *                       NaN for a row that holds a value that is not finite, which then reads back as NaN
+ *   k_levels, v_levels  [heads, 16] of type t, ascending, finite; in units of the largest magnitude, so within [-1, 1]
+ *                       (v_levels: below 65504 in any case, they are multiplied as fp16)
+ * t is FK_F16 or FK_BF16; page_size a power of two from 16 to 65536; d a multiple of 32 up to 256; 1 <= heads <= 256;
+ * pages * page_size below 2^40.  A slot is page * page_size + place in the page.  (Levels out of order give other ids, never
+ * other memory.)
+ */
+typedef struct {
+    void *k_codes, *v_codes;
+    void *k_scale, *v_scale;
+    const void *k_levels, *v_levels;
+    int64_t pages;
+    int page_size, heads, d;
+    fk_dtype t;
+} fk_kv_cache;
+
+/*
+ * T new tokens: keys and values into their slots, keys and queries turned by the angles of their positions.
+ *   k, v       device, rows [T, heads, d] of type t at element strides (token, head); channels are contiguous.  Strides
+ *              are any number of elements, so the parts of a joint projection's output are taken as they lie.
+ *   slots      device, [T] int64; a token whose slot is outside the cache (-1, say) is left out.  Tokens of one call
+ *              have different slots.
+ *   rot        channels that turn, a multiple of 16 up to d; 0 = none (cos_sin and positions are then unused).  Pairs (p, p + rot/2), or
+ *              (2p, 2p + 1) with interleaved != 0: y_i = x_i cos - x_j sin, y_j = x_j cos + x_i sin, products and
+ *              sums in fp32, the result rounded to t.  A key is rounded before it is coded: the cache codes the row
+ *              that an uncoded cache would hold.
+ *   cos_sin    device, [max_pos, rot] float: rot/2 cosines, then rot/2 sines of each position
+ *   positions  device, [T] int32, clamped to [0, max_pos)
+ *   q, q_out   device or both NULL: queries [T, q_heads, d] at strides like k, and where the turned ones go, [T, q_heads, d]
+ *              contiguous (q_out may be q where q is contiguous)
+ * Of two levels at the same distance the lower is taken.  Distances are compared in fp32 with one rounding.
+ */
+fk_status fk_kv_append(const fk_kv_cache* cache, const void* k, int64_t k_token_stride, int64_t k_head_stride,
+                       const void* v, int64_t v_token_stride, int64_t v_head_stride, const int64_t* slots, int64_t T,
+                       const float* cos_sin, const int32_t* positions, int64_t max_pos, int rot, int interleaved,
+                       const void* q, int64_t q_token_stride, int64_t q_head_stride, int q_heads, void* q_out,
+                       void* stream);
+
+/*
+ * Rows of the cache as the values they stand for, level * scale rounded to t.
+ *   slots         device, [T] int64; a slot outside the cache gives zeros
+ *   k_out, v_out  device out, [T, heads, d] of type t; either may be NULL
+ */
+fk_status fk_kv_read(const fk_kv_cache* cache, const int64_t* slots, int64_t T, void* k_out, void* v_out, void* stream);
+
+/*
+ * softmax(scale * q.K) V over the cache, for B sequences.
+ *   q        device, [Tq, q_heads, d] of type t at element strides (token, head); q_heads is a multiple of
+ *            cache->heads, query head i reads cache head i / (q_heads / heads)
+ *   pages    device, [B, max_pages] int32: the pages of each sequence in order (entries outside the cache are clamped into it)
+ *   lens     device, [B] int32: tokens of each sequence in the cache (at most max_pages * page_size count)
+ *   q_start  device, [B+1] int32, ascending from 0: the queries of sequence b are tokens q_start[b] .. q_start[b+1] of q,
+ *            at most max_q of them; NULL: max_q each, Tq = B * max_q.  They are the last ones of
+ *            the sequence: query i of n sits at position lens[b] - n + i.
+ *   causal   0: a query sees all tokens of its sequence; otherwise those up to its own position
+ *   window   > 0: only tokens less than `window` before its own position; 0: no such limit
+ *   max_pages * page_size at most 2^30
+ *   max_len  an upper bound of lens, from which the work is divided; 0 = max_pages * page_size.  (Longer sequences
+ *            are still attended to in full, less evenly divided.)
+ *   out      device out, [Tq, q_heads, d] of type t; zeros for a query that sees no token
+ *   lse      device out or NULL, [Tq, q_heads] float: log of the sum of exp(scale * q.K); -inf where nothing is seen
+ * Scores, softmax statistics and sums are fp32; the weights exp(score - max) * v_scale are rounded to fp16 (11 bits, relative to a
+ * power of two near the sequence's largest v_scale) for the product with the values.  Results do not depend on the order of
+ * workgroups.  What lies in the cache beyond a sequence's length or outside its window has no influence, NaN included.
+ */
+fk_status fk_kv_attend(const fk_kv_cache* cache, const void* q, int64_t q_token_stride, int64_t q_head_stride,
+                       int q_heads, int64_t Tq, const int32_t* pages, int max_pages, const int32_t* lens,
+                       const int32_t* q_start, int B, int max_q, int64_t max_len, float scale, int causal, int window,
+                       void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+/* Device bytes that fk_kv_attend needs in ws (256-byte aligned, contents undefined before and after); 0 if unsupported.  Of the cache
+ * only the sizes and t are read; max_len >= 1. */
+size_t fk_kv_workspace_bytes(const fk_kv_cache* cache, int q_heads, int64_t Tq, int B, int max_q, int64_t max_len);
+
 #ifdef __cplusplus
 }
 #endif

@@ -22,8 +22,14 @@ _STATUS = {0: "FK_OK", 1: "FK_EINVAL", 2: "FK_EUNSUPPORTED", 3: "FK_EWORKSPACE",
 EXPORTS = ("fk_last_error", "fk_workspace_bytes", "fk_assign", "fk_sort_inverse", "fk_update",
            "fk_lloyd_iter", "fk_lloyd_ooc", "fk_ooc_workspace_bytes", "fk_stage_timer_start",
            "fk_stage_timer_stop", "fk_plan", "fk_set_option", "fk_standard_assign",
-           "fk_standard_update", "fk_assign_static", "fk_assign_static_limit")
+           "fk_standard_update", "fk_assign_static", "fk_assign_static_limit", "fk_kv_append", "fk_kv_read",
+           "fk_kv_attend", "fk_kv_workspace_bytes")
 STAGES = ("assign", "sort", "reduce", "finalize")
+
+
+class _KVCacheStruct(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k_codes", "v_codes", "k_scale", "v_scale", "k_levels", "v_levels")] + [
+        ("pages", ctypes.c_int64), ("page_size", ctypes.c_int), ("heads", ctypes.c_int), ("d", ctypes.c_int), ("t", ctypes.c_int)]
 
 
 class FlashKMError(RuntimeError):
@@ -69,6 +75,16 @@ def lib() -> ctypes.CDLL:
         L.fk_standard_assign.argtypes = [vp, vp, vp, vp, i32, i64, i32, i32, i32, vp, sz, vp]
         L.fk_standard_update.restype = i32
         L.fk_standard_update.argtypes = [vp, vp, vp, vp, vp, vp, i32, i64, i32, i32, i32, vp]
+        cache = ctypes.POINTER(_KVCacheStruct)
+        L.fk_kv_append.restype = i32
+        L.fk_kv_append.argtypes = [cache, vp, i64, i64, vp, i64, i64, vp, i64, vp, vp, i64, i32, i32, vp, i64, i64, i32, vp, vp]
+        L.fk_kv_read.restype = i32
+        L.fk_kv_read.argtypes = [cache, vp, i64, vp, vp, vp]
+        L.fk_kv_attend.restype = i32
+        L.fk_kv_attend.argtypes = [cache, vp, i64, i64, i32, i64, vp, i32, vp, vp, i32, i32, i64, ctypes.c_float, i32, i32, vp, vp,
+                                   vp, sz, vp]
+        L.fk_kv_workspace_bytes.restype = sz
+        L.fk_kv_workspace_bytes.argtypes = [cache, i32, i64, i32, i32, i64]
         L.fk_plan.restype = i32
         L.fk_plan.argtypes = [i32, i64, i32, i32, i32, ctypes.c_char_p, sz]
         L.fk_set_option.restype = i32
@@ -279,3 +295,139 @@ def fk_standard_update(X, assign, C_prev_f32, *, sums=None):
                                     _ptr(counts), _ptr(sums), B, N, d, K, _DTYPE[X.dtype],
                                     _stream(X.device)))
     return C_out, counts
+
+
+class KVCache:
+    """A paged key/value cache in 4 bits over the caller's tensors (see fk_kv_cache in include/flashkm.h).
+
+    codes [pages, heads, page_size, d/2] uint8, scales [pages, heads, page_size] and levels [heads, 16] of one 16-bit type, the
+    levels ascending.  `KVCache.empty` allocates the codes and scales."""
+
+    def __init__(self, k_codes, v_codes, k_scale, v_scale, k_levels, v_levels):
+        if k_codes.dim() != 4:
+            raise ValueError("k_codes must be [pages, heads, page_size, d/2]")
+        P, H, S, half = k_codes.shape
+        t = k_scale.dtype
+        if t not in _DTYPE:
+            raise ValueError(f"k_scale must be a type of the library, got {t}")
+        _dev(k_codes, "k_codes", torch.uint8)
+        _dev(v_codes, "v_codes", torch.uint8, k_codes.shape)
+        _dev(k_scale, "k_scale", t, (P, H, S)); _dev(v_scale, "v_scale", t, (P, H, S))
+        _dev(k_levels, "k_levels", t, (H, 16)); _dev(v_levels, "v_levels", t, (H, 16))
+        tensors = (k_codes, v_codes, k_scale, v_scale, k_levels, v_levels)
+        if any(x.device != k_codes.device for x in tensors):
+            raise ValueError("the cache's tensors must be on one device")
+        self.k_codes, self.v_codes, self.k_scale, self.v_scale, self.k_levels, self.v_levels = tensors
+        self.pages, self.heads, self.page_size, self.d, self.dtype, self.device = P, H, S, 2 * half, t, k_codes.device
+        self._struct = _KVCacheStruct(*(x.data_ptr() for x in tensors), P, S, H, 2 * half, _DTYPE[t])
+
+    @classmethod
+    def empty(cls, pages: int, page_size: int, k_levels, v_levels, d: int) -> "KVCache":
+        H, dev, t = k_levels.shape[0], k_levels.device, k_levels.dtype
+        codes = [torch.zeros((pages, H, page_size, d // 2), dtype=torch.uint8, device=dev) for _ in range(2)]
+        scale = [torch.zeros((pages, H, page_size), dtype=t, device=dev) for _ in range(2)]
+        return cls(*codes, *scale, k_levels, v_levels)
+
+
+def _rows(t: torch.Tensor, name: str, cache: KVCache, heads=None):
+    """Rows [T, heads, d] whose channels are contiguous -> (pointer, token stride, head stride)."""
+    if not t.is_cuda or t.device != cache.device:
+        raise ValueError(f"{name} must be on the cache's device")
+    if t.dtype != cache.dtype:
+        raise ValueError(f"{name} must be {cache.dtype}, got {t.dtype}")
+    if t.dim() != 3 or t.shape[2] != cache.d or (heads is not None and t.shape[1] != heads):
+        raise ValueError(f"{name} must have shape [T, {heads or 'heads'}, {cache.d}], got {tuple(t.shape)}")
+    if t.stride(2) != 1:
+        raise ValueError(f"{name}: the channels of a row must be contiguous")
+    return _ptr(t), t.stride(0), t.stride(1)
+
+
+def _ints(t, name: str, cache: KVCache, dtype, shape):
+    if t.device != cache.device:
+        raise ValueError(f"{name} must be on the cache's device")
+    return _ptr(_dev(t, name, dtype, shape))
+
+
+def fk_kv_append(cache: KVCache, k, v, slots, *, positions=None, cos_sin=None, interleaved: bool = False, q=None, q_out=None):
+    """k, v [T, heads, d] into the slots [T] int64 of the cache, keys turned by the angles of positions [T] int32 (cos_sin
+    [max_pos, rot] float32: cosines, then sines); q [T, q_heads, d] is turned likewise and returned (None without q)."""
+    T = k.shape[0]
+    kr, vr = _rows(k, "k", cache, cache.heads), _rows(v, "v", cache, cache.heads)
+    if v.shape[0] != T:
+        raise ValueError("k and v must have the same number of tokens")
+    sl = _ints(slots, "slots", cache, torch.int64, (T,))
+    rot, max_pos, cs, ps = 0, 0, None, None
+    if cos_sin is not None:
+        if cos_sin.dim() != 2:
+            raise ValueError("cos_sin must be [max_pos, rot]")
+        max_pos, rot = cos_sin.shape
+    if rot:
+        if positions is None:
+            raise ValueError("cos_sin needs positions")
+        cs = _ints(cos_sin, "cos_sin", cache, torch.float32, None)
+        ps = _ints(positions, "positions", cache, torch.int32, (T,))
+    qr, heads = (None, 0, 0), 0
+    if q is not None:
+        heads = q.shape[1] if q.dim() == 3 else 0
+        qr = _rows(q, "q", cache)
+        if q.shape[0] != T:
+            raise ValueError("q and k must have the same number of tokens")
+        if q_out is None:
+            q_out = torch.empty((T, heads, cache.d), dtype=q.dtype, device=q.device)
+        _ints(q_out, "q_out", cache, cache.dtype, (T, heads, cache.d))
+    _check(lib().fk_kv_append(ctypes.byref(cache._struct), *kr, *vr, sl, T, cs, ps, max_pos, rot, int(interleaved), *qr, heads,
+                              _ptr(q_out) if q is not None else None, _stream(cache.device)))
+    return q_out if q is not None else None
+
+
+def fk_kv_read(cache: KVCache, slots, *, k_out=None, v_out=None):
+    """The rows at slots [T] int64 as the values they stand for -> (k, v) [T, heads, d]."""
+    T = slots.shape[0]
+    sl = _ints(slots, "slots", cache, torch.int64, (T,))
+    shape = (T, cache.heads, cache.d)
+    k_out = torch.empty(shape, dtype=cache.dtype, device=cache.device) if k_out is None else k_out
+    v_out = torch.empty(shape, dtype=cache.dtype, device=cache.device) if v_out is None else v_out
+    _check(lib().fk_kv_read(ctypes.byref(cache._struct), sl, T, _ints(k_out, "k_out", cache, cache.dtype, shape),
+                            _ints(v_out, "v_out", cache, cache.dtype, shape), _stream(cache.device)))
+    return k_out, v_out
+
+
+def fk_kv_workspace_bytes(cache: KVCache, B: int, q_heads: int, Tq: int, max_q: int, max_len: int) -> int:
+    return int(lib().fk_kv_workspace_bytes(ctypes.byref(cache._struct), q_heads, Tq, B, max_q, max_len))
+
+
+def make_kv_workspace(cache: KVCache, B: int, q_heads: int, Tq: int, max_q: int, max_len: int) -> torch.Tensor:
+    n = fk_kv_workspace_bytes(cache, B, q_heads, Tq, max_q, max_len)
+    if n == 0:
+        raise FlashKMError(2, f"unsupported attention: {lib().fk_last_error().decode()}")
+    return torch.empty(n, dtype=torch.uint8, device=cache.device)
+
+
+def fk_kv_attend(cache: KVCache, q, pages, lens, *, q_start=None, max_q=None, max_len: int = 0, scale=None, causal: bool = True,
+                 window: int = 0, lse: bool = False, ws=None, out=None):
+    """q [Tq, q_heads, d] against the cached sequences: pages [B, max_pages] int32, lens [B] int32.  The queries of sequence b are
+    q[q_start[b] : q_start[b+1]] (q_start [B+1] int32 with the most of a sequence in max_q; without it max_q each, one by default), the
+    last tokens of the sequence.  -> out [Tq, q_heads, d] (and the logarithm of the sums [Tq, q_heads] float32)."""
+    qr = _rows(q, "q", cache)
+    Tq, heads = q.shape[0], q.shape[1]
+    if pages.dim() != 2:
+        raise ValueError("pages must be [B, max_pages]")
+    B, max_pages = pages.shape
+    pg = _ints(pages, "pages", cache, torch.int32, (B, max_pages))
+    ln = _ints(lens, "lens", cache, torch.int32, (B,))
+    if max_q is None:
+        if q_start is not None:
+            raise ValueError("q_start needs max_q")
+        max_q = max(1, Tq // B)
+    qs = None if q_start is None else _ints(q_start, "q_start", cache, torch.int32, (B + 1,))
+    max_len = max_len or max_pages * cache.page_size
+    if ws is None:
+        ws = make_kv_workspace(cache, B, heads, Tq, max_q, max_len)
+    _dev(ws, "ws", torch.uint8)
+    out = torch.empty((Tq, heads, cache.d), dtype=q.dtype, device=q.device) if out is None else out
+    le = torch.empty((Tq, heads), dtype=torch.float32, device=q.device) if lse else None
+    _check(lib().fk_kv_attend(ctypes.byref(cache._struct), *qr, heads, Tq, pg, max_pages, ln, qs, B, max_q, max_len,
+                              float(cache.d ** -0.5 if scale is None else scale), int(causal), window,
+                              _ints(out, "out", cache, cache.dtype, (Tq, heads, cache.d)), _ptr(le), _ptr(ws), ws.numel(),
+                              _stream(cache.device)))
+    return (out, le) if lse else out
