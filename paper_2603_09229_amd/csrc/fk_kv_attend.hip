@@ -25,7 +25,7 @@
 
 namespace fk {
 
-constexpr float kSlack = 8.f;            // log2
+constexpr float kSlack = 8.f;            // in powers of two
 constexpr float kScaleSlack = 64.f;
 constexpr float kNone = -3.402823466e38f;  // maximum of a row that has seen nothing
 constexpr int kJoinWaves = 8;            // waves of a workgroup that share the rows
@@ -46,6 +46,18 @@ __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
     return (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)lo) | ((uint32_t)__builtin_bit_cast(uint16_t, (_Float16)hi) << 16);
 }
 
+__device__ __forceinline__ uint32_t pk_max_u16(uint32_t a, uint32_t b) {
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+
+// kScaleSlack units as two numbers of type t, at most the largest finite one
+template <bool BF>
+__device__ __forceinline__ uint32_t limit_of(float unit) {
+    const uint32_t l = float_to_lp_any(fminf(kScaleSlack * unit, BF ? 0x1.fep127f : 65504.f), BF);
+    return l | l << 16;
+}
+
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 struct AttendArgs {
@@ -54,7 +66,8 @@ struct AttendArgs {
     int group;                 // query heads to a cache head
     int splits, row_blocks;
     int chunk;
-    float scale_log2;
+    float scale_log2;          // positive, so that scores that are not seen stay -inf:
+    uint32_t flip;             // the signs of the queries' channels are flipped instead
 };
 
 // Blocks of the values' channels by the number of bytes that a lane takes of each: ND bytes in pieces of 4, 2 and 1 (powers of two, so
@@ -96,25 +109,42 @@ struct Reader {
         return min(max(p, 0), (int)A.c.pages - 1);
     }
 
-    __device__ __forceinline__ void load(Codes<ND>& f, int at, int page0, int page1) const {
+    // first rows of a step's halves
+    __device__ __forceinline__ void rows_of(int64_t (&row)[2], int at, int page0, int page1) const {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             const int from = min(at + 16 * u, last_half) & ((1 << A.c.page_shift) - 1);
-            const int64_t row = (((int64_t)(u ? page1 : page0) * A.c.heads + h) << A.c.page_shift) + from;
-            const uint8_t* kc = A.c.k_codes + row * (16 * ND) + n * (16 * ND) + q * (4 * ND);
-            const uint8_t* vc = A.c.v_codes + row * (16 * ND) + q * 4 * (16 * ND);
-            f.ks[u] = *(const uintx2*)(A.c.k_scale + row + 4 * q);
-            f.vs[u] = *(const uintx2*)(A.c.v_scale + row + 4 * q);
-            __builtin_memcpy(f.k[u], __builtin_assume_aligned(kc, 4), 4 * ND);
-            using P = Pieces<ND>;
+            row[u] = (((int64_t)(u ? page1 : page0) * A.c.heads + h) << A.c.page_shift) + from;
+        }
+    }
+    // (bases are the same in all lanes, what differs between lanes is an unsigned 32-bit offset: one address register for all loads
+    // of a kind)
+    __device__ __forceinline__ void load_keys(Codes<ND>& f, const int64_t (&row)[2]) const {
+        const uint32_t of = n * (16 * ND) + q * (4 * ND);
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
+        for (int u = 0; u < 2; ++u) __builtin_memcpy(f.k[u], __builtin_assume_aligned(A.c.k_codes + row[u] * (16 * ND) + of, 4), 4 * ND);
+    }
+    __device__ __forceinline__ void load_scales(Codes<ND>& f, const int64_t (&row)[2]) const {
+        const uint32_t of = 8 * q;
 #pragma unroll
-                for (int p = 0; p < P::count; ++p) {
-                    const uint8_t* at = vc + r * (16 * ND) + 16 * P::before(p) + n * P::width(p);
+        for (int u = 0; u < 2; ++u) {
+            f.ks[u] = *(const uintx2*)((const uint8_t*)(A.c.k_scale + row[u]) + of);
+            f.vs[u] = *(const uintx2*)((const uint8_t*)(A.c.v_scale + row[u]) + of);
+        }
+    }
+    __device__ __forceinline__ void load_values(Codes<ND>& f, const int64_t (&row)[2]) const {
+        using P = Pieces<ND>;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int p = 0; p < P::count; ++p) {
+                const uint32_t of = q * 4 * (16 * ND) + n * P::width(p);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const uint8_t* at = A.c.v_codes + row[u] * (16 * ND) + of + (r * (16 * ND) + 16 * P::before(p));
                     f.v[u][r][p] = P::width(p) == 4 ? *(const uint32_t*)at : P::width(p) == 2 ? *(const uint16_t*)at : *at;
                 }
-        }
+            }
     }
 };
 
@@ -128,8 +158,9 @@ __device__ __forceinline__ uint32_t pair_of(const uint8_t* lds, uint32_t word, i
 }
 
 template <bool BF, int ND, int NT, bool JOIN>
-__global__ __launch_bounds__(64 * (JOIN ? kJoinWaves : kOwnWaves)) void kv_attend_kernel(AttendArgs A) {
-    extern __shared__ __align__(16) uint8_t lds[];
+__global__ __launch_bounds__(64 * (JOIN ? kJoinWaves : kOwnWaves), JOIN && NT == 1 && ND <= 4 ? 4 : 1) void kv_attend_kernel(AttendArgs A) {
+    // (a fixed size, so that the compiler knows the table's address and leaves it to the instruction's offset)
+    __shared__ __align__(16) uint8_t lds[kTableBytes + (JOIN ? 2 * kJoinWaves * 16 * NT * 4 : 0)];
     using P = Pieces<ND>;
     constexpr int R = 16 * NT, S = 2 * ND, W = JOIN ? kJoinWaves : 1, THREADS = 64 * (JOIN ? kJoinWaves : kOwnWaves);
     const int b = blockIdx.z, h = blockIdx.y, split = blockIdx.x % A.splits, rb = blockIdx.x / A.splits;
@@ -159,10 +190,14 @@ __global__ __launch_bounds__(64 * (JOIN ? kJoinWaves : kOwnWaves)) void kv_atten
     Reader<BF, ND> in{A, a.pages + (int64_t)b * a.max_pages, h, max(hi - 1, 0) & ~15, lane, n, q};
     int ahead = 0;                                                // lane l: page of half l % 2 of step l / 2 of this batch
     auto pages_from = [&](int step) { return in.page_of(mine + (step + lane / 2) * W * kStep + (lane & 1) * 16); };
-    Codes<ND> next;
+    Codes<ND> f;                                                  // the step's, refilled piece by piece as it is used up
+    int64_t row[2];
     if (steps) {
         ahead = pages_from(0);
-        in.load(next, mine, __builtin_amdgcn_readlane(ahead, 0), __builtin_amdgcn_readlane(ahead, 1));
+        in.rows_of(row, mine, __builtin_amdgcn_readlane(ahead, 0), __builtin_amdgcn_readlane(ahead, 1));
+        in.load_keys(f, row);
+        in.load_scales(f, row);
+        in.load_values(f, row);
     }
 
     {   // the table of pairs
@@ -187,7 +222,7 @@ __global__ __launch_bounds__(64 * (JOIN ? kJoinWaves : kOwnWaves)) void kv_atten
 #pragma unroll
         for (int k = 0; k < ND; ++k) {
             Q[c][k] = uintx4{0, 0, 0, 0};
-            if (live) Q[c][k] = *(const uintx4_any*)(at + 8 * k);
+            if (live) Q[c][k] = *(const uintx4_any*)(at + 8 * k) ^ A.flip;
         }
         const int pos = len - nq + i;
         see_hi[c] = !live ? 0 : a.causal ? min(len, pos + 1) : len;
@@ -203,18 +238,17 @@ __global__ __launch_bounds__(64 * (JOIN ? kJoinWaves : kOwnWaves)) void kv_atten
 #pragma unroll
         for (int s = 0; s < S; ++s) O[s][c] = floatx4{0, 0, 0, 0};
     }
-    float unit = 0.f, per_unit = 1.f;                             // power of two near the largest s'
+    float unit = 0.f, per_unit = 1.f;                             // of the weights: a power of two near the largest s'
+    uint32_t limit2 = 0;                                          // kScaleSlack units as type t, twice
     const uint32_t copy = (lane & 31) * 4;
     __syncthreads();
 
     for (int it = 0; it < steps; ++it) {
         const int at = mine + it * W * kStep;
-        const Codes<ND> f = next;
-        if (it + 1 < steps) {
-            if ((it + 1) % kPagesAhead == 0) ahead = pages_from(it + 1);
-            const int l = 2 * ((it + 1) % kPagesAhead);
-            in.load(next, at + W * kStep, __builtin_amdgcn_readlane(ahead, l), __builtin_amdgcn_readlane(ahead, l + 1));
-        }
+        if ((it + 1) % kPagesAhead == 0) ahead = pages_from(it + 1);
+        const int l = 2 * ((it + 1) % kPagesAhead);
+        // rows of the next step (after the last one: of the sequence's end, not used)
+        in.rows_of(row, at + W * kStep, __builtin_amdgcn_readlane(ahead, l), __builtin_amdgcn_readlane(ahead, l + 1));
 
         floatx4 X[2][NT];
 #pragma unroll
@@ -231,66 +265,82 @@ __global__ __launch_bounds__(64 * (JOIN ? kJoinWaves : kOwnWaves)) void kv_atten
 #pragma unroll
                 for (int c = 0; c < NT; ++c) X[u][c] = mfma16<BF>(op, Q[c][k], X[u][c]);
             }
+        in.load_keys(f, row);
 
-        const bool whole = at + kStep <= whole_end && at >= whole_from;
-        // scales of the lane's 8 tokens; those that no row sees count as none
-        float ks[8], vs[8], most = 0.f;
+        float vs[8], x[NT][8], peak[NT];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            ks[e] = scale_at<BF>(f.ks[e / 4], e & 3) * A.scale_log2;
             vs[e] = scale_at<BF>(f.vs[e / 4], e & 3);
-            const int token = at + 16 * (e / 4) + 4 * q + (e & 3);
-            if (!whole && (token < lo || token >= hi)) vs[e] = 0.f;
-            most = fmaxf(most, vs[e]);
+#pragma unroll
+            for (int c = 0; c < NT; ++c) x[c][e] = X[e / 4][c][e & 3] * scale_at<BF>(f.ks[e / 4], e & 3);
         }
-        if (__any(most > kScaleSlack * unit)) {
-            most = fmaxf(most, __shfl_xor(most, 16));
-            most = fmaxf(most, __shfl_xor(most, 32));
-            const float to = fminf(__uint_as_float(max(__float_as_uint(most) & 0x7f800000u, 0x00800000u)), 0x1p127f);
-            const float ratio = unit / to;
-            unit = to;
-            per_unit = 1.f / to;
-#pragma unroll
-            for (int c = 0; c < NT; ++c)
-#pragma unroll
-                for (int s = 0; s < S; ++s) O[s][c] *= ratio;
-        }
-
-        uintx4 w[NT];
-#pragma unroll
-        for (int c = 0; c < NT; ++c) {
-            float x[8], peak = kNone;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = X[e / 4][c][e & 3] * ks[e];
-            if (!whole) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int token = at + 16 * (e / 4) + 4 * q + (e & 3);
-                    if (token < see_lo[c] || token >= see_hi[c]) x[e] = -INFINITY;
-                }
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) peak = fmaxf(peak, x[e]);
-            if (__any(peak > top[c] + kSlack)) {
-                peak = fmaxf(peak, __shfl_xor(peak, 16));
-                peak = fmaxf(peak, __shfl_xor(peak, 32));
-                peak = fmaxf(peak, top[c]);
-                const float shrink = exp2_fast(top[c] - peak);
-                top[c] = peak;
-                sum[c] *= shrink;
-#pragma unroll
-                for (int s = 0; s < S; ++s) O[s][c] *= shrink;
-            }
-            float y[8];
+        if (at + kStep > whole_end || at < whole_from) {          // some row does not see all of these tokens
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float p = exp2_fast(x[e] - top[c]);
-                sum[c] += p;
-                y[e] = p * (vs[e] * per_unit);
-                if (!whole && x[e] == -INFINITY) y[e] = 0.f;      // NaN scales of what is not seen
+                const int token = at + 4 * q + 16 * (e / 4) + (e & 3);
+                // A scale that is not finite reaches the rows that see it by way of their scores; where none does, or the tokens are
+                // past the end, it may be anything.
+                const bool bad = !(vs[e] <= 3.402823466e38f);
+#pragma unroll
+                for (int c = 0; c < NT; ++c)
+                    x[c][e] = token < see_lo[c] || token >= see_hi[c] ? -INFINITY : bad ? NAN : x[c][e];
+                if (bad || token < lo || token >= hi) vs[e] = 0.f;
+            }
+        }
+        // The largest scale of the values against the limit, two at a time as 16-bit integers (they are positive), and the scores
+        // against the maxima.
+        uint32_t most2 = limit2;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) most2 = pk_max_u16(most2, f.vs[u][j]);
+        in.load_scales(f, row);
+        bool move = most2 != limit2;
+#pragma unroll
+        for (int c = 0; c < NT; ++c) {
+            peak[c] = kNone;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) peak[c] = fmaxf(peak[c], x[c][e]);
+            move |= fmaf(peak[c], A.scale_log2, -top[c]) > kSlack;
+        }
+        if (__any(move)) {
+            float most = 0.f, ratio = 1.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) most = fmaxf(most, vs[e]);
+            most = fmaxf(most, __shfl_xor(most, 16));
+            most = fmaxf(most, __shfl_xor(most, 32));
+            if (most > kScaleSlack * unit) {                      // the same in all lanes
+                const float to = fminf(__uint_as_float(max(__float_as_uint(most) & 0x7f800000u, 0x00800000u)), 0x1p126f);
+                ratio = unit / to;
+                unit = to;
+                per_unit = 1.f / to;
+                limit2 = limit_of<BF>(unit);
             }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) w[c][j] = pack_half2(y[2 * j], y[2 * j + 1]);
+            for (int c = 0; c < NT; ++c) {
+                float to = fmaxf(peak[c], __shfl_xor(peak[c], 16));
+                to = fmaxf(to, __shfl_xor(to, 32));
+                // (a column's maximum moves by its own scores alone: what other rows see has no part in its rounding)
+                to = fmaf(to, A.scale_log2, -top[c]) > kSlack ? to * A.scale_log2 : top[c];
+                const float shrink = exp2_fast(top[c] - to);
+                top[c] = to;
+                sum[c] *= shrink;
+#pragma unroll
+                for (int s = 0; s < S; ++s) O[s][c] *= shrink * ratio;
+            }
+        }
+        uintx4 w[NT];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) vs[e] *= per_unit;
+#pragma unroll
+        for (int c = 0; c < NT; ++c) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                x[c][e] = exp2_fast(fmaf(x[c][e], A.scale_log2, -top[c]));
+                sum[c] += x[c][e];
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[c][j] = pack_half2(x[c][2 * j] * vs[2 * j], x[c][2 * j + 1] * vs[2 * j + 1]);
         }
 
 #pragma unroll
@@ -314,6 +364,7 @@ __global__ __launch_bounds__(64 * (JOIN ? kJoinWaves : kOwnWaves)) void kv_atten
                     for (int c = 0; c < NT; ++c) O[s][c] = mfma16<false>(op, w[c], O[s][c]);
                 }
         }
+        in.load_values(f, row);
     }
 
 #pragma unroll
@@ -463,15 +514,8 @@ KVPlan choose_kv_plan(const KVView& c, int q_heads, int B, int max_q, int64_t re
 
 template <bool BF, int ND, int NT, bool JOIN>
 static fk_status launch_form(const AttendArgs& A, hipStream_t s) {
-    static PerDeviceInt allowed;
     const int waves = JOIN ? kJoinWaves : kOwnWaves;
-    const size_t lds = kTableBytes + (JOIN ? (size_t)2 * kJoinWaves * 16 * NT * 4 : 0);
-    const auto kern = kv_attend_kernel<BF, ND, NT, JOIN>;
-    if (!allowed.get()) {
-        FK_HIP(hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-        allowed.set(1);
-    }
-    kern<<<dim3(A.row_blocks * A.splits, A.c.heads, A.a.B), 64 * waves, lds, s>>>(A);
+    kv_attend_kernel<BF, ND, NT, JOIN><<<dim3(A.row_blocks * A.splits, A.c.heads, A.a.B), 64 * waves, 0, s>>>(A);
     FK_HIP(hipGetLastError());
     if (JOIN && A.splits > 1) {
         kv_join_kernel<BF, ND, NT><<<dim3(A.row_blocks * 2 * ND * NT, A.c.heads, A.a.B), 256, 0, s>>>(A);
@@ -505,7 +549,7 @@ static fk_status launch_type(const AttendArgs& A, const KVPlan& p, hipStream_t s
 }
 
 fk_status launch_kv_attend(const KVView& c, const KVAttend& a, const KVPlan& p, hipStream_t s) {
-    const AttendArgs A{c, a, a.q_heads / c.heads, p.splits, p.row_blocks, (int)p.chunk, a.scale * 1.44269504088896341f};
+    const AttendArgs A{c, a, a.q_heads / c.heads, p.splits, p.row_blocks, (int)p.chunk, fmaxf(fabsf(a.scale) * 1.44269504088896341f, 1e-37f), a.scale < 0.f ? 0x80008000u : 0u};
     return c.bf ? launch_type<true>(A, p, s) : launch_type<false>(A, p, s);
 }
 
