@@ -320,6 +320,7 @@ class KVCache:
         self.k_codes, self.v_codes, self.k_scale, self.v_scale, self.k_levels, self.v_levels = tensors
         self.pages, self.heads, self.page_size, self.d, self.dtype, self.device = P, H, S, 2 * half, t, k_codes.device
         self._struct = _KVCacheStruct(*(x.data_ptr() for x in tensors), P, S, H, 2 * half, _DTYPE[t])
+        self._ref, self._index = ctypes.byref(self._struct), k_codes.get_device()
 
     @classmethod
     def empty(cls, pages: int, page_size: int, k_levels, v_levels, d: int) -> "KVCache":
@@ -329,71 +330,79 @@ class KVCache:
         return cls(*codes, *scale, k_levels, v_levels)
 
 
-def _rows(t: torch.Tensor, name: str, cache: KVCache, heads=None):
+# A call that serves one token is over on the GPU in a few microseconds, so that the checks below count: each asks a tensor's
+# properties in one expression (pointers go to ctypes as plain numbers), and only a tensor that fails is looked at closer.
+def _rows(t: torch.Tensor, name: str, cache: KVCache, T, heads):
     """Rows [T, heads, d] whose channels are contiguous -> (pointer, token stride, head stride)."""
-    if not t.is_cuda or t.device != cache.device:
-        raise ValueError(f"{name} must be on the cache's device")
+    if t.dtype is cache.dtype and t.get_device() == cache._index and t.shape == (T, heads, cache.d):
+        a, b, c = t.stride()
+        if c == 1:
+            return t.data_ptr(), a, b
+        raise ValueError(f"{name}: the channels of a row must be contiguous")
     if t.dtype != cache.dtype:
         raise ValueError(f"{name} must be {cache.dtype}, got {t.dtype}")
-    if t.dim() != 3 or t.shape[2] != cache.d or (heads is not None and t.shape[1] != heads):
-        raise ValueError(f"{name} must have shape [T, {heads or 'heads'}, {cache.d}], got {tuple(t.shape)}")
-    if t.stride(2) != 1:
-        raise ValueError(f"{name}: the channels of a row must be contiguous")
-    return _ptr(t), t.stride(0), t.stride(1)
-
-
-def _ints(t, name: str, cache: KVCache, dtype, shape):
-    if t.device != cache.device:
+    if t.get_device() != cache._index:
         raise ValueError(f"{name} must be on the cache's device")
-    return _ptr(_dev(t, name, dtype, shape))
+    raise ValueError(f"{name} must have shape {(T, heads, cache.d)}, got {tuple(t.shape)}")
+
+
+def _array(t: torch.Tensor, name: str, cache: KVCache, dtype, shape) -> int:
+    """A contiguous tensor on the cache's device -> pointer."""
+    if t.dtype is dtype and t.shape == shape and t.get_device() == cache._index and t.is_contiguous():
+        return t.data_ptr()
+    if t.get_device() != cache._index:
+        raise ValueError(f"{name} must be on the cache's device")
+    return _dev(t, name, dtype, shape).data_ptr()
+
+
+def _raw_stream(cache: KVCache) -> int:
+    return torch._C._cuda_getCurrentRawStream(cache._index)
 
 
 def fk_kv_append(cache: KVCache, k, v, slots, *, positions=None, cos_sin=None, interleaved: bool = False, q=None, q_out=None):
     """k, v [T, heads, d] into the slots [T] int64 of the cache, keys turned by the angles of positions [T] int32 (cos_sin
     [max_pos, rot] float32: cosines, then sines); q [T, q_heads, d] is turned likewise and returned (None without q)."""
-    T = k.shape[0]
-    kr, vr = _rows(k, "k", cache, cache.heads), _rows(v, "v", cache, cache.heads)
-    if v.shape[0] != T:
-        raise ValueError("k and v must have the same number of tokens")
-    sl = _ints(slots, "slots", cache, torch.int64, (T,))
-    rot, max_pos, cs, ps = 0, 0, None, None
+    T, H, d = k.shape[0], cache.heads, cache.d
+    kp, kt, kh = _rows(k, "k", cache, T, H)
+    vp, vt, vh = _rows(v, "v", cache, T, H)
+    rot = max_pos = cs = ps = 0
     if cos_sin is not None:
         if cos_sin.dim() != 2:
             raise ValueError("cos_sin must be [max_pos, rot]")
         max_pos, rot = cos_sin.shape
-    if rot:
-        if positions is None:
-            raise ValueError("cos_sin needs positions")
-        cs = _ints(cos_sin, "cos_sin", cache, torch.float32, None)
-        ps = _ints(positions, "positions", cache, torch.int32, (T,))
-    qr, heads = (None, 0, 0), 0
+        if rot:
+            if positions is None:
+                raise ValueError("cos_sin needs positions")
+            cs = _array(cos_sin, "cos_sin", cache, torch.float32, cos_sin.shape)
+            ps = _array(positions, "positions", cache, torch.int32, (T,))
+    qp = qt = qh = heads = qo = 0
     if q is not None:
-        heads = q.shape[1] if q.dim() == 3 else 0
-        qr = _rows(q, "q", cache)
-        if q.shape[0] != T:
-            raise ValueError("q and k must have the same number of tokens")
+        heads = q.shape[1]
+        qp, qt, qh = _rows(q, "q", cache, T, heads)
         if q_out is None:
-            q_out = torch.empty((T, heads, cache.d), dtype=q.dtype, device=q.device)
-        _ints(q_out, "q_out", cache, cache.dtype, (T, heads, cache.d))
-    _check(lib().fk_kv_append(ctypes.byref(cache._struct), *kr, *vr, sl, T, cs, ps, max_pos, rot, int(interleaved), *qr, heads,
-                              _ptr(q_out) if q is not None else None, _stream(cache.device)))
+            q_out = torch.empty((T, heads, d), dtype=cache.dtype, device=cache.device)
+        qo = _array(q_out, "q_out", cache, cache.dtype, (T, heads, d))
+    _check(lib().fk_kv_append(cache._ref, kp, kt, kh, vp, vt, vh, _array(slots, "slots", cache, torch.int64, (T,)), T, cs, ps,
+                              max_pos, rot, interleaved, qp, qt, qh, heads, qo, _raw_stream(cache)))
     return q_out if q is not None else None
 
 
 def fk_kv_read(cache: KVCache, slots, *, k_out=None, v_out=None):
     """The rows at slots [T] int64 as the values they stand for -> (k, v) [T, heads, d]."""
     T = slots.shape[0]
-    sl = _ints(slots, "slots", cache, torch.int64, (T,))
     shape = (T, cache.heads, cache.d)
-    k_out = torch.empty(shape, dtype=cache.dtype, device=cache.device) if k_out is None else k_out
-    v_out = torch.empty(shape, dtype=cache.dtype, device=cache.device) if v_out is None else v_out
-    _check(lib().fk_kv_read(ctypes.byref(cache._struct), sl, T, _ints(k_out, "k_out", cache, cache.dtype, shape),
-                            _ints(v_out, "v_out", cache, cache.dtype, shape), _stream(cache.device)))
+    if k_out is None:
+        k_out = torch.empty(shape, dtype=cache.dtype, device=cache.device)
+    if v_out is None:
+        v_out = torch.empty(shape, dtype=cache.dtype, device=cache.device)
+    _check(lib().fk_kv_read(cache._ref, _array(slots, "slots", cache, torch.int64, (T,)), T,
+                            _array(k_out, "k_out", cache, cache.dtype, shape), _array(v_out, "v_out", cache, cache.dtype, shape),
+                            _raw_stream(cache)))
     return k_out, v_out
 
 
 def fk_kv_workspace_bytes(cache: KVCache, B: int, q_heads: int, Tq: int, max_q: int, max_len: int) -> int:
-    return int(lib().fk_kv_workspace_bytes(ctypes.byref(cache._struct), q_heads, Tq, B, max_q, max_len))
+    return int(lib().fk_kv_workspace_bytes(cache._ref, q_heads, Tq, B, max_q, max_len))
 
 
 def make_kv_workspace(cache: KVCache, B: int, q_heads: int, Tq: int, max_q: int, max_len: int) -> torch.Tensor:
@@ -408,26 +417,26 @@ def fk_kv_attend(cache: KVCache, q, pages, lens, *, q_start=None, max_q=None, ma
     """q [Tq, q_heads, d] against the cached sequences: pages [B, max_pages] int32, lens [B] int32.  The queries of sequence b are
     q[q_start[b] : q_start[b+1]] (q_start [B+1] int32 with the most of a sequence in max_q; without it max_q each, one by default), the
     last tokens of the sequence.  -> out [Tq, q_heads, d] (and the logarithm of the sums [Tq, q_heads] float32)."""
-    qr = _rows(q, "q", cache)
-    Tq, heads = q.shape[0], q.shape[1]
-    if pages.dim() != 2:
-        raise ValueError("pages must be [B, max_pages]")
+    Tq, heads, _ = q.shape
+    qp, qt, qh = _rows(q, "q", cache, Tq, heads)
     B, max_pages = pages.shape
-    pg = _ints(pages, "pages", cache, torch.int32, (B, max_pages))
-    ln = _ints(lens, "lens", cache, torch.int32, (B,))
+    qs = 0
     if max_q is None:
         if q_start is not None:
             raise ValueError("q_start needs max_q")
         max_q = max(1, Tq // B)
-    qs = None if q_start is None else _ints(q_start, "q_start", cache, torch.int32, (B + 1,))
-    max_len = max_len or max_pages * cache.page_size
+    if q_start is not None:
+        qs = _array(q_start, "q_start", cache, torch.int32, (B + 1,))
+    if not max_len:
+        max_len = max_pages * cache.page_size
     if ws is None:
         ws = make_kv_workspace(cache, B, heads, Tq, max_q, max_len)
-    _dev(ws, "ws", torch.uint8)
-    out = torch.empty((Tq, heads, cache.d), dtype=q.dtype, device=q.device) if out is None else out
-    le = torch.empty((Tq, heads), dtype=torch.float32, device=q.device) if lse else None
-    _check(lib().fk_kv_attend(ctypes.byref(cache._struct), *qr, heads, Tq, pg, max_pages, ln, qs, B, max_q, max_len,
-                              float(cache.d ** -0.5 if scale is None else scale), int(causal), window,
-                              _ints(out, "out", cache, cache.dtype, (Tq, heads, cache.d)), _ptr(le), _ptr(ws), ws.numel(),
-                              _stream(cache.device)))
+    if out is None:
+        out = torch.empty((Tq, heads, cache.d), dtype=cache.dtype, device=cache.device)
+    le = torch.empty((Tq, heads), dtype=torch.float32, device=cache.device) if lse else None
+    _check(lib().fk_kv_attend(cache._ref, qp, qt, qh, heads, Tq, _array(pages, "pages", cache, torch.int32, (B, max_pages)), max_pages,
+                              _array(lens, "lens", cache, torch.int32, (B,)), qs, B, max_q, max_len,
+                              cache.d ** -0.5 if scale is None else scale, causal, window,
+                              _array(out, "out", cache, cache.dtype, (Tq, heads, cache.d)), le.data_ptr() if lse else 0,
+                              _array(ws, "ws", cache, torch.uint8, ws.shape), ws.numel(), _raw_stream(cache)))
     return (out, le) if lse else out

@@ -20,6 +20,8 @@
 //
 // The running maximum is only moved when a score passes it by 2^kSlack, the weights' scale (a power of two near the largest s') when one
 // passes that by 2^kScaleSlack: the sums are then multiplied once.  Weights stay below 2^15 and fit fp16.
+#include <algorithm>
+
 #include "fk_device.h"
 #include "fk_kv.h"
 
@@ -32,6 +34,7 @@ constexpr int kJoinWaves = 8;            // waves of a workgroup that share the 
 constexpr int kOwnWaves = 4;             // waves of a workgroup with rows of their own
 constexpr int kStep = 32;                // tokens a wave takes at a time
 constexpr size_t kTableBytes = 65536;
+constexpr int kMostSplits = 256;          // of one row block's tokens
 constexpr int kPagesAhead = 32;          // steps whose pages a wave holds in one register (two halves each)
 
 template <bool BF>
@@ -42,8 +45,9 @@ __device__ __forceinline__ floatx4 mfma16(uintx4 a, uintx4 b, floatx4 c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, a), __builtin_bit_cast(half8, b), c, 0, 0, 0);
 }
 
+__device__ __forceinline__ uint32_t float_to_half(float f) { return __builtin_bit_cast(uint16_t, (_Float16)f); }
 __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
-    return (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)lo) | ((uint32_t)__builtin_bit_cast(uint16_t, (_Float16)hi) << 16);
+    return float_to_half(lo) | float_to_half(hi) << 16;
 }
 
 __device__ __forceinline__ uint32_t pk_max_u16(uint32_t a, uint32_t b) {
@@ -200,14 +204,15 @@ __global__ __launch_bounds__(64 * (JOIN ? kJoinWaves : kOwnWaves), JOIN && NT ==
         in.load_values(f, row);
     }
 
-    {   // the table of pairs
-        const uint16_t *kl = A.c.k_levels + h * 16, *vl = A.c.v_levels + h * 16;
-        for (int i = threadIdx.x; i < (int)kTableBytes / 16; i += THREADS) {
-            const int code = i / 16;
-            uint32_t pair;
-            if ((i & 15) < 8) pair = kl[code & 15] | ((uint32_t)kl[code >> 4] << 16);
-            else pair = pack_half2(lp_to_float(vl[code & 15], BF), lp_to_float(vl[code >> 4], BF));
-            ((uintx4*)lds)[i] = uintx4{pair, pair, pair, pair};
+    {   // The table of pairs.  Lanes 0..15 hold the keys' levels, lanes 16..31 the values'; sixteen pieces of 16 bytes make a row.
+        const uint16_t level = ((lane & 16) ? A.c.v_levels : A.c.k_levels)[h * 16 + (lane & 15)];
+        const uint32_t mine = (lane & 16) ? float_to_half(lp_to_float(level, BF)) : level;
+        const int side = (lane & 8) * 2;
+#pragma unroll
+        for (int i = 0; i < (int)kTableBytes / 16 / THREADS; ++i) {
+            const int at = i * THREADS + threadIdx.x, code = at / 16;
+            const uint32_t pair = (uint32_t)__shfl((int)mine, side + (code & 15)) | ((uint32_t)__shfl((int)mine, side + (code >> 4)) << 16);
+            ((uintx4*)lds)[at] = uintx4{pair, pair, pair, pair};
         }
     }
 
@@ -436,6 +441,7 @@ __global__ __launch_bounds__(64 * (JOIN ? kJoinWaves : kOwnWaves), JOIN && NT ==
 #pragma unroll
                 for (int j = 1; j < NT; ++j) { tc = c == j ? t[j] : tc; lc = c == j ? l[j] : lc; }
                 if (partial) {
+                    if (row0 + c * 16 + n >= rows) continue;
                     ((floatx4*)(part + 2 * R))[(s * NT + c) * 64 + lane] = o;
                     if (s == 0 && q == 0) {
                         part[c * 16 + n] = tc;
@@ -449,11 +455,14 @@ __global__ __launch_bounds__(64 * (JOIN ? kJoinWaves : kOwnWaves), JOIN && NT ==
     }
 }
 
-// Joins the splits of one subtile of one row block: its four waves take every fourth split, then add up what they have.
+// Joins the splits of one subtile of one row block.  All their maxima and sums are read at once, 16 columns by 32 splits, and become the
+// splits' factors in LDS; then each of the eight waves adds every eighth split's products, and the first wave what they have.
+constexpr int kJoinThreads = 512;
 template <bool BF, int ND, int NT>
-__global__ __launch_bounds__(256) void kv_join_kernel(AttendArgs A) {
-    constexpr int R = 16 * NT;
-    __shared__ floatx4 swap[4][64];
+__global__ __launch_bounds__(kJoinThreads) void kv_join_kernel(AttendArgs A) {
+    constexpr int R = 16 * NT, WAVES = kJoinThreads / 64, LANES = kJoinThreads / 16;
+    __shared__ floatx4 swap[WAVES][64];
+    __shared__ float factor[kMostSplits][16], most[WAVES][16], all[WAVES][16];
     const KVAttend& a = A.a;
     const int b = blockIdx.z, h = blockIdx.y, tile = blockIdx.x % (2 * ND * NT), rb = blockIdx.x / (2 * ND * NT);
     const int s = tile / NT, c = tile % NT;
@@ -462,7 +471,7 @@ __global__ __launch_bounds__(256) void kv_join_kernel(AttendArgs A) {
     const int q0 = a.q_start ? min(max(a.q_start[b], 0), (int)a.Tq) : b * a.max_q;
     const int nq = a.q_start ? min(min(max(a.q_start[b + 1] - q0, 0), a.max_q), (int)a.Tq - q0) : a.max_q;
     const int rows = nq * A.group, row0 = rb * R;
-    if (row0 >= rows) return;
+    if (row0 + c * 16 >= rows) return;
     const int i0 = row0 / A.group, i1 = (min(row0 + R, rows) - 1) / A.group;
     const int hi = a.causal ? max(min(len, len - nq + i1 + 1), 0) : len;
     const int lo = (a.window ? max(0, len - nq + i0 - a.window + 1) : 0) & ~(kStep - 1);
@@ -471,21 +480,48 @@ __global__ __launch_bounds__(256) void kv_join_kernel(AttendArgs A) {
     const int64_t stride = R * (32 * ND + 2);
     const float* part = a.part + (((int64_t)b * A.c.heads + h) * A.row_blocks + rb) * A.splits * stride;
     const int col = c * 16 + n;
-    float t = kNone, l = 0.f;
-    for (int i = 0; i < parts; ++i) t = fmaxf(t, part[i * stride + col]);
-    for (int i = 0; i < parts; ++i) l += part[i * stride + R + col] * exp2_fast(part[i * stride + col] - t);
-    floatx4 o = {0, 0, 0, 0};
-    for (int i = wave; i < parts; i += 4) {
-        const float f = exp2_fast(part[i * stride + col] - t);
-        o += f * ((const floatx4*)(part + i * stride + 2 * R))[(s * NT + c) * 64 + lane];
+    const bool live = row0 + col < rows;
+
+    constexpr int EACH = kMostSplits / LANES;
+    float tops[EACH], sums[EACH], t = kNone, l = 0.f;
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) {
+        const int i = k * LANES + wave * 4 + q;
+        tops[k] = i < parts && live ? part[i * stride + col] : kNone;
+        sums[k] = i < parts && live ? part[i * stride + R + col] : 0.f;
+        t = fmaxf(t, tops[k]);
     }
+    t = fmaxf(t, __shfl_xor(t, 16));
+    t = fmaxf(t, __shfl_xor(t, 32));
+    if (q == 0) most[wave][n] = t;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) t = fmaxf(t, most[w][n]);
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) {
+        const float f = exp2_fast(tops[k] - t);
+        factor[k * LANES + wave * 4 + q][n] = f;
+        l += sums[k] * f;
+    }
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    if (q == 0) all[wave][n] = l;
+    __syncthreads();
+
+    floatx4 o = {0, 0, 0, 0};
+    const floatx4* from = (const floatx4*)(part + 2 * R) + (s * NT + c) * 64 + lane;
+    if (live)
+#pragma unroll 8
+        for (int i = wave; i < parts; i += WAVES) o += factor[i][n] * *(const floatx4*)((const float*)from + i * stride);
     swap[wave][lane] = o;
     __syncthreads();
-    if (wave) return;
+    if (wave || !live) return;
+    l = 0.f;
 #pragma unroll
-    for (int w = 1; w < 4; ++w) o += swap[w][lane];
+    for (int w = 0; w < WAVES; ++w) l += all[w][n];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) o += swap[w][lane];
     const int row = row0 + col, i = row / A.group, g = row - i * A.group;
-    if (row >= rows) return;
     const int64_t at = (int64_t)(q0 + i) * a.q_heads + h * A.group + g;
     const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
 #pragma unroll
@@ -498,7 +534,7 @@ KVPlan choose_kv_plan(const KVView& c, int q_heads, int B, int max_q, int64_t re
     const int64_t rows = (int64_t)max_q * group;
     const int most = c.d <= 128 ? 4 : 2;                         // tiles of a wave
     KVPlan p;
-    p.join = rows <= 16 * most;
+    p.join = rows <= 16 * most || (int64_t)B * c.heads * cdiv(rows, 16 * most * kOwnWaves) < device_cu_count();
     p.tiles = !p.join ? most : rows <= 16 ? 1 : rows <= 32 ? 2 : most;
     p.row_blocks = (int)cdiv(rows, 16 * p.tiles * (p.join ? 1 : kOwnWaves));
     p.splits = 1;
@@ -506,7 +542,7 @@ KVPlan choose_kv_plan(const KVView& c, int q_heads, int B, int max_q, int64_t re
     if (p.join) {
         const int64_t wg = kJoinWaves * kStep, slots = (int64_t)device_cu_count() * 2, blocks = (int64_t)B * c.heads * p.row_blocks;
         const int64_t want = blocks >= slots ? 1 : slots / blocks, steps = cdiv(reach, wg);
-        p.splits = (int)(want < steps ? want : steps);
+        p.splits = (int)std::min({want, steps, (int64_t)kMostSplits});
         if (p.splits > 1) p.chunk = cdiv(steps, p.splits) * wg;
     }
     return p;
@@ -518,7 +554,7 @@ static fk_status launch_form(const AttendArgs& A, hipStream_t s) {
     kv_attend_kernel<BF, ND, NT, JOIN><<<dim3(A.row_blocks * A.splits, A.c.heads, A.a.B), 64 * waves, 0, s>>>(A);
     FK_HIP(hipGetLastError());
     if (JOIN && A.splits > 1) {
-        kv_join_kernel<BF, ND, NT><<<dim3(A.row_blocks * 2 * ND * NT, A.c.heads, A.a.B), 256, 0, s>>>(A);
+        kv_join_kernel<BF, ND, NT><<<dim3(A.row_blocks * 2 * ND * NT, A.c.heads, A.a.B), kJoinThreads, 0, s>>>(A);
         FK_HIP(hipGetLastError());
     }
     return FK_OK;
