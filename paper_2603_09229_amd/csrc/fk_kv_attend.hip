@@ -33,7 +33,6 @@ constexpr float kNone = -3.402823466e38f;  // maximum of a row that has seen not
 constexpr int kJoinWaves = 8;            // waves of a workgroup that share the rows
 constexpr int kOwnWaves = 4;             // waves of a workgroup with rows of their own
 constexpr int kStep = 32;                // tokens a wave takes at a time
-constexpr size_t kTableBytes = 65536;
 constexpr int kMostSplits = 256;          // of one row block's tokens
 constexpr int kPagesAhead = 32;          // steps whose pages a wave holds in one register (two halves each)
 
@@ -100,6 +99,33 @@ __device__ __forceinline__ int channel_of(int s, int m) {
     return 2 * (16 * P::before(p) + m * P::width(p) + (byte - P::before(p))) + (s & 1);
 }
 
+// The largest of 16 lanes (not NaN), in all of them; lane exchanges of the vector ALU, a few cycles each where LDS takes a hundred
+template <int CTRL>
+__device__ __forceinline__ float max_with(float v) {
+    return fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false)));
+}
+__device__ __forceinline__ float row_max(float v) {
+    v = max_with<0xB1>(v);                                        // lane ^ 1
+    v = max_with<0x4E>(v);                                        // lane ^ 2
+    v = max_with<0x141>(v);                                       // mirrored in 8
+    return max_with<0x140>(v);                                    // mirrored in 16
+}
+__device__ __forceinline__ float lane_of(float v, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane)); }
+
+// An address that is the same in all lanes, as scalar registers: loads then take a 32-bit offset of the lane and need no 64-bit vector
+// addition each.
+typedef __attribute__((address_space(1))) const uint8_t* Base;
+__device__ __forceinline__ Base base_of(const void* p, int64_t bytes) {
+    const uint64_t v = (uint64_t)p + bytes;
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((int)(uint32_t)v), hi = __builtin_amdgcn_readfirstlane((int)(uint32_t)(v >> 32));
+    return (Base)((uint64_t)hi << 32 | lo);
+}
+template <class T>
+__device__ __forceinline__ T load_at(Base base, uint32_t offset) {
+    typedef __attribute__((address_space(1))) const T* At;
+    return *(At)(base + offset);
+}
+
 template <bool BF, int ND>
 struct Reader {
     const AttendArgs& A;
@@ -121,61 +147,267 @@ struct Reader {
             row[u] = (((int64_t)(u ? page1 : page0) * A.c.heads + h) << A.c.page_shift) + from;
         }
     }
-    // (bases are the same in all lanes, what differs between lanes is an unsigned 32-bit offset: one address register for all loads
-    // of a kind)
     __device__ __forceinline__ void load_keys(Codes<ND>& f, const int64_t (&row)[2]) const {
         const uint32_t of = n * (16 * ND) + q * (4 * ND);
-#pragma unroll
-        for (int u = 0; u < 2; ++u) __builtin_memcpy(f.k[u], __builtin_assume_aligned(A.c.k_codes + row[u] * (16 * ND) + of, 4), 4 * ND);
-    }
-    __device__ __forceinline__ void load_scales(Codes<ND>& f, const int64_t (&row)[2]) const {
-        const uint32_t of = 8 * q;
+        typedef uint32_t uintx3 __attribute__((ext_vector_type(3)));
+        typedef uint32_t uintx4_at4 __attribute__((ext_vector_type(4), aligned(4)));
+        typedef uint32_t uintx3_at4 __attribute__((ext_vector_type(3), aligned(4)));
+        typedef uint32_t uintx2_at4 __attribute__((ext_vector_type(2), aligned(4)));
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            f.ks[u] = *(const uintx2*)((const uint8_t*)(A.c.k_scale + row[u]) + of);
-            f.vs[u] = *(const uintx2*)((const uint8_t*)(A.c.v_scale + row[u]) + of);
+            const Base base = base_of(A.c.k_codes, row[u] * (16 * ND));
+            if constexpr (ND >= 4) {
+                const uintx4 v = load_at<uintx4_at4>(base, of);
+                f.k[u][0] = v[0]; f.k[u][1] = v[1]; f.k[u][2] = v[2]; f.k[u][3] = v[3];
+            }
+            constexpr int done = ND & 4 || ND == 8 ? 4 : 0;
+            if constexpr (ND == 8) {
+                const uintx4 v = load_at<uintx4_at4>(base, of + 16);
+                f.k[u][4] = v[0]; f.k[u][5] = v[1]; f.k[u][6] = v[2]; f.k[u][7] = v[3];
+            } else if constexpr (ND - done == 3) {
+                const uintx3 v = load_at<uintx3_at4>(base, of + 4 * done);
+                f.k[u][done] = v[0]; f.k[u][done + 1] = v[1]; f.k[u][done + 2] = v[2];
+            } else if constexpr (ND - done == 2) {
+                const uintx2 v = load_at<uintx2_at4>(base, of + 4 * done);
+                f.k[u][done] = v[0]; f.k[u][done + 1] = v[1];
+            } else if constexpr (ND - done == 1) {
+                f.k[u][done] = load_at<uint32_t>(base, of + 4 * done);
+            }
+        }
+    }
+    __device__ __forceinline__ void load_scales(Codes<ND>& f, const int64_t (&row)[2]) const {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            f.ks[u] = load_at<uintx2>(base_of(A.c.k_scale, row[u] * 2), 8 * q);
+            f.vs[u] = load_at<uintx2>(base_of(A.c.v_scale, row[u] * 2), 8 * q);
         }
     }
     __device__ __forceinline__ void load_values(Codes<ND>& f, const int64_t (&row)[2]) const {
         using P = Pieces<ND>;
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int u = 0; u < 2; ++u) {
+            const Base base = base_of(A.c.v_codes, row[u] * (16 * ND));
 #pragma unroll
             for (int p = 0; p < P::count; ++p) {
                 const uint32_t of = q * 4 * (16 * ND) + n * P::width(p);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const uint8_t* at = A.c.v_codes + row[u] * (16 * ND) + of + (r * (16 * ND) + 16 * P::before(p));
-                    f.v[u][r][p] = P::width(p) == 4 ? *(const uint32_t*)at : P::width(p) == 2 ? *(const uint16_t*)at : *at;
+                    const int more = r * (16 * ND) + 16 * P::before(p);
+                    f.v[u][r][p] = P::width(p) == 4 ? load_at<uint32_t>(base, of + more)
+                                 : P::width(p) == 2 ? load_at<uint16_t>(base, of + more) : load_at<uint8_t>(base, of + more);
                 }
             }
+        }
     }
 };
 
 template <bool BF>
 __device__ __forceinline__ float scale_at(uintx2 s, int r) { return lp_to_float((uint16_t)(s[r / 2] >> 16 * (r & 1)), BF); }
 
-// Two levels of each of four bytes: byte b of the words, in order
-template <int OFFSET>
-__device__ __forceinline__ uint32_t pair_of(const uint8_t* lds, uint32_t word, int b, uint32_t copy) {
-    return *(const uint32_t*)(lds + __builtin_amdgcn_perm(word, copy, 0x0c0c0400u | (uint32_t)b << 8) + OFFSET);
+// A table of pairs of levels in LDS: 256 rows of COPIES pairs of the keys' levels and as many of the values'.
+template <int COPIES>
+struct Table {
+    static constexpr int bytes = 256 * COPIES * 8;
+    static_assert(COPIES == 32 || COPIES == 16, "rows of 256 bytes, or two to that");
+
+    // what `pair` takes as `copy`: the lane's copy in a row of 256 bytes
+    static __device__ __forceinline__ uint32_t copy_of(int lane) { return (lane % COPIES) * 4 * (32 / COPIES); }
+
+    // the pair of byte b of the word
+    template <bool VALUES>
+    static __device__ __forceinline__ uint32_t pair(const uint8_t* lds, uint32_t word, int b, uint32_t copy) {
+        const uint32_t at = __builtin_amdgcn_perm(word, copy, 0x0c0c0400u | (uint32_t)b << 8) / (32 / COPIES);
+        return *(const uint32_t*)(lds + at + (VALUES ? COPIES * 4 : 0));
+    }
+
+    // Lanes 0..15 hold the keys' levels, lanes 16..31 the values'.
+    template <bool BF, int THREADS>
+    static __device__ __forceinline__ void fill(uint8_t* lds, const KVView& c, int h, int lane) {
+        constexpr int pieces = COPIES / 2, keys = pieces / 2;     // of 16 bytes: of a row, and of its keys' part
+        const uint16_t level = ((lane & 16) ? c.v_levels : c.k_levels)[h * 16 + (lane & 15)];
+        const uint32_t mine = (lane & 16) ? float_to_half(lp_to_float(level, BF)) : level;
+        const int side = lane & keys ? 16 : 0;
+#pragma unroll
+        for (int i = 0; i < bytes / 16 / THREADS; ++i) {
+            const int at = i * THREADS + threadIdx.x, code = at / pieces;
+            const uint32_t pair = (uint32_t)__shfl((int)mine, side + (code & 15)) | ((uint32_t)__shfl((int)mine, side + (code >> 4)) << 16);
+            ((uintx4*)lds)[at] = uintx4{pair, pair, pair, pair};
+        }
+    }
+};
+
+// Where a sequence's queries are and what they see.
+struct Place {
+    int len, q0, nq, rows;
+    __device__ __forceinline__ Place(const KVAttend& a, const KVView& c, int group, int b) {
+        len = min(max(a.lens[b], 0), a.max_pages << c.page_shift);
+        q0 = a.q_start ? min(max(a.q_start[b], 0), (int)a.Tq) : b * a.max_q;
+        nq = a.q_start ? min(min(max(a.q_start[b + 1] - q0, 0), a.max_q), (int)a.Tq - q0) : a.max_q;
+        rows = nq * group;
+    }
+};
+
+// The tokens that a wave's rows see: all of [lo, hi) is seen by some row; the row of column c, at position pos[c], sees those of
+// [0, hi) that are more than `before` and at most `after` from it.
+template <int NT>
+struct Seen {
+    int lo, hi, before, after, pos[NT];
+};
+
+// Query rows from row0 on: the operand, and where the columns' rows are.
+template <int ND, int NT>
+__device__ __forceinline__ void load_queries(const AttendArgs& A, const Place& p, int h, int row0, int n, int q, uintx4 (&Q)[NT][ND],
+                                             Seen<NT>& seen) {
+    const KVAttend& a = A.a;
+#pragma unroll
+    for (int c = 0; c < NT; ++c) {
+        const int row = row0 + c * 16 + n, i = row / A.group, g = row - i * A.group;
+        const bool live = row < p.rows;
+        const uint16_t* at = a.q.at + (int64_t)(p.q0 + i) * a.q.token + (int64_t)(h * A.group + g) * a.q.head + q * (8 * ND);
+#pragma unroll
+        for (int k = 0; k < ND; ++k) {
+            Q[c][k] = uintx4{0, 0, 0, 0};
+            if (live) Q[c][k] = *(const uintx4_any*)(at + 8 * k) ^ A.flip;
+        }
+        seen.pos[c] = p.len - p.nq + i;
+    }
+    seen.after = a.causal ? 0 : INT32_MAX;
+    seen.before = a.window ? -a.window : INT32_MIN;
 }
 
+// 1 / sum, 0 for a row that has seen nothing; and its lse (top in powers of two)
+__device__ __forceinline__ float inverse(float sum) { return sum > 0.f || sum != sum ? 1.f / sum : 0.f; }
+__device__ __forceinline__ float lse_of(float top, float sum) {
+    return sum > 0.f || sum != sum ? (top + __log2f(sum)) * 0.6931471805599453f : -INFINITY;
+}
+
+// Maxima, sums and the weights' unit of a wave's rows; a lane keeps its column's, its own tokens' share of the sum.
+template <int NT, int S>
+struct Softmax {
+    float top[NT], sum[NT];    // reference of the exponents (0 before anything is seen), sum of the exponentials
+    float unit = 0.f, per_unit = 1.f;
+    float limit = 0.f;         // kScaleSlack units
+
+    __device__ __forceinline__ Softmax() {
+#pragma unroll
+        for (int c = 0; c < NT; ++c) top[c] = sum[c] = 0.f;
+    }
+
+    // One step's scores X (before the keys' scales ks, which come times scale log2 e) become weights w; products O move with their
+    // reference.  The lane's e-th score is of token first + 16 (e / 4) + e % 4, scale_of(e) its values' scale and most the largest of
+    // the step where every row sees all of it.
+    template <class ScaleOf>
+    __device__ __forceinline__ void step(const floatx4 (&X)[2][NT], const float (&ks)[8], ScaleOf scale_of, float most, bool masked,
+                                         const Seen<NT>& seen, int first, floatx4 (&O)[S][NT], uintx4 (&w)[NT]) {
+        float x[NT][8], peak[NT];
+        uint32_t dead = 0;                                        // bit e: a scale that must not be multiplied
+#pragma unroll
+        for (int c = 0; c < NT; ++c)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[c][e] = fmaf(X[e / 4][c][e & 3], ks[e], -top[c]);
+        if (masked) {
+            most = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int token = first + 16 * (e / 4) + (e & 3);
+                // A scale that is not finite reaches the rows that see it by way of their scores; where none does, or the tokens are
+                // past the end, it may be anything.
+                const float v = scale_of(e);
+                const bool bad = !(v <= 3.402823466e38f), out = bad || token < seen.lo || token >= seen.hi;
+#pragma unroll
+                for (int c = 0; c < NT; ++c)
+                    x[c][e] = token >= seen.hi || token - seen.pos[c] > seen.after || token - seen.pos[c] <= seen.before ? -INFINITY
+                            : bad ? NAN : x[c][e];
+                dead |= out ? 1u << e : 0u;
+                most = fmaxf(most, out ? 0.f : v);
+            }
+        }
+        bool move = most > limit;
+#pragma unroll
+        for (int c = 0; c < NT; ++c) {
+            peak[c] = x[c][0];
+#pragma unroll
+            for (int e = 1; e < 8; ++e) peak[c] = fmaxf(peak[c], x[c][e]);
+            move |= peak[c] > (sum[c] == 0.f ? -3.402823466e38f : kSlack);
+        }
+        if (__any(move)) {
+            float ratio = 1.f;
+            most = fmaxf(most, __shfl_xor(most, 16));
+            most = fmaxf(most, __shfl_xor(most, 32));
+            if (most > limit) {                                   // the same in all lanes
+                const float to = fminf(__uint_as_float(max(__float_as_uint(most) & 0x7f800000u, 0x00800000u)), 0x1p126f);
+                ratio = unit / to;
+                unit = to;
+                per_unit = 1.f / to;
+                limit = fminf(kScaleSlack * to, 3.402823466e38f);
+            }
+#pragma unroll
+            for (int c = 0; c < NT; ++c) {
+                // (a column's reference moves by its own scores alone: what other rows see has no part in its rounding)
+                float by = fmaxf(peak[c], __shfl_xor(peak[c], 16)), had = sum[c] + __shfl_xor(sum[c], 16);
+                by = fmaxf(by, __shfl_xor(by, 32));
+                had += __shfl_xor(had, 32);
+                by = by > (had == 0.f ? -3.402823466e38f : kSlack) ? by : 0.f;
+                const float shrink = exp2_fast(-by);
+                top[c] += by;
+                if (had != 0.f) sum[c] *= shrink;
+                const float f = had != 0.f ? shrink * ratio : 0.f;
+#pragma unroll
+                for (int s = 0; s < S; ++s) O[s][c] *= f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[c][e] -= by;
+            }
+        }
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = scale_of(e) * per_unit;
+        if (masked) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = dead >> e & 1 ? 0.f : v[e];
+        }
+#pragma unroll
+        for (int c = 0; c < NT; ++c) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                x[c][e] = exp2_fast(x[c][e]);
+                sum[c] += x[c][e];
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[c][j] = pack_half2(x[c][2 * j] * v[2 * j], x[c][2 * j + 1] * v[2 * j + 1]);
+        }
+    }
+
+    // The columns' sums, and products in units of the values
+    __device__ __forceinline__ void finish(floatx4 (&O)[S][NT]) {
+#pragma unroll
+        for (int c = 0; c < NT; ++c) {
+            sum[c] += __shfl_xor(sum[c], 16);
+            sum[c] += __shfl_xor(sum[c], 32);
+#pragma unroll
+            for (int s = 0; s < S; ++s) O[s][c] *= unit;
+        }
+    }
+};
+
+// JOIN: the waves of a workgroup share the rows and divide the tokens, each takes every kJoinWaves-th step (and workgroups may divide them
+// further); otherwise each wave has rows of its own and takes all steps that they see.  Codes go straight from the cache into operands.
 template <bool BF, int ND, int NT, bool JOIN>
-__global__ __launch_bounds__(64 * (JOIN ? kJoinWaves : kOwnWaves), JOIN && NT == 1 && ND <= 4 ? 4 : 1) void kv_attend_kernel(AttendArgs A) {
+__global__ __launch_bounds__(64 * (JOIN ? kJoinWaves : kOwnWaves), JOIN ? (NT == 1 && ND <= 4 ? 4 : 1) : 2)
+void kv_attend_kernel(AttendArgs A) {
     // (a fixed size, so that the compiler knows the table's address and leaves it to the instruction's offset)
-    __shared__ __align__(16) uint8_t lds[kTableBytes + (JOIN ? 2 * kJoinWaves * 16 * NT * 4 : 0)];
+    using T = Table<32>;
+    __shared__ __align__(16) uint8_t lds[T::bytes + (JOIN ? 2 * kJoinWaves * 16 * NT * 4 : 0)];
     using P = Pieces<ND>;
     constexpr int R = 16 * NT, S = 2 * ND, W = JOIN ? kJoinWaves : 1, THREADS = 64 * (JOIN ? kJoinWaves : kOwnWaves);
-    const int b = blockIdx.z, h = blockIdx.y, split = blockIdx.x % A.splits, rb = blockIdx.x / A.splits;
+    // (rows of their own: the blocks with the most tokens first)
+    const int blocks = A.c.heads * A.a.B;
+    const int h = JOIN ? blockIdx.y : blockIdx.x % A.c.heads, b = JOIN ? blockIdx.z : blockIdx.x / A.c.heads % A.a.B;
+    const int split = JOIN ? blockIdx.x % A.splits : 0, rb = JOIN ? blockIdx.x / A.splits : A.row_blocks - 1 - blockIdx.x / blocks;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63, n = lane & 15, q = lane >> 4;
     const KVAttend& a = A.a;
 
-    const int len = min(max(a.lens[b], 0), a.max_pages << A.c.page_shift);
-    const int q0 = a.q_start ? min(max(a.q_start[b], 0), (int)a.Tq) : b * a.max_q;
-    const int nq = a.q_start ? min(min(max(a.q_start[b + 1] - q0, 0), a.max_q), (int)a.Tq - q0) : a.max_q;
-    const int rows = nq * A.group;
-    const int row0 = (JOIN ? rb : rb * kOwnWaves + wave) * R;
+    const Place at(a, A.c, A.group, b);
+    const int rows = at.rows, len = at.len, q0 = at.q0, nq = at.nq, row0 = (JOIN ? rb : rb * kOwnWaves + wave) * R;
     if ((JOIN ? row0 : rb * kOwnWaves * R) >= rows) return;       // the whole workgroup
 
     // tokens that the wave's rows see
@@ -183,8 +415,8 @@ __global__ __launch_bounds__(64 * (JOIN ? kJoinWaves : kOwnWaves), JOIN && NT ==
     const int p0 = len - nq + i0, p1 = len - nq + i1;
     const int hi = row0 >= rows ? 0 : a.causal ? max(min(len, p1 + 1), 0) : len;
     const int lo = a.window ? max(0, p0 - a.window + 1) : 0;
-    const int first = (lo & ~(kStep - 1)) + split * A.chunk;
-    const int end = split == A.splits - 1 ? hi : min(hi, first + A.chunk);
+    const int first = (lo & ~(kStep - 1)) + (JOIN ? split * A.chunk : 0);
+    const int end = !JOIN || split == A.splits - 1 ? hi : min(hi, first + A.chunk);
     if (JOIN && split > 0 && first >= hi) return;                 // the whole workgroup
     // a step is whole where every row sees all of its tokens
     const int whole_end = a.causal ? min(len, p0 + 1) : len, whole_from = a.window ? p1 - a.window + 1 : 0;
@@ -204,56 +436,28 @@ __global__ __launch_bounds__(64 * (JOIN ? kJoinWaves : kOwnWaves), JOIN && NT ==
         in.load_values(f, row);
     }
 
-    {   // The table of pairs.  Lanes 0..15 hold the keys' levels, lanes 16..31 the values'; sixteen pieces of 16 bytes make a row.
-        const uint16_t level = ((lane & 16) ? A.c.v_levels : A.c.k_levels)[h * 16 + (lane & 15)];
-        const uint32_t mine = (lane & 16) ? float_to_half(lp_to_float(level, BF)) : level;
-        const int side = (lane & 8) * 2;
-#pragma unroll
-        for (int i = 0; i < (int)kTableBytes / 16 / THREADS; ++i) {
-            const int at = i * THREADS + threadIdx.x, code = at / 16;
-            const uint32_t pair = (uint32_t)__shfl((int)mine, side + (code & 15)) | ((uint32_t)__shfl((int)mine, side + (code >> 4)) << 16);
-            ((uintx4*)lds)[at] = uintx4{pair, pair, pair, pair};
-        }
-    }
-
-    // query rows: operand, and the tokens that each column's row sees
+    T::fill<BF, THREADS>(lds, A.c, h, lane);
     uintx4 Q[NT][ND];
-    int see_lo[NT], see_hi[NT];
-#pragma unroll
-    for (int c = 0; c < NT; ++c) {
-        const int row = row0 + c * 16 + n, i = row / A.group, g = row - i * A.group;
-        const bool live = row < rows;
-        const uint16_t* at = a.q.at + (int64_t)(q0 + i) * a.q.token + (int64_t)(h * A.group + g) * a.q.head + q * (8 * ND);
-#pragma unroll
-        for (int k = 0; k < ND; ++k) {
-            Q[c][k] = uintx4{0, 0, 0, 0};
-            if (live) Q[c][k] = *(const uintx4_any*)(at + 8 * k) ^ A.flip;
-        }
-        const int pos = len - nq + i;
-        see_hi[c] = !live ? 0 : a.causal ? min(len, pos + 1) : len;
-        see_lo[c] = a.window ? pos - a.window + 1 : 0;
-    }
+    Seen<NT> seen;
+    seen.lo = lo;
+    seen.hi = hi;
+    load_queries<ND, NT>(A, at, h, row0, n, q, Q, seen);
 
     floatx4 O[S][NT];
-    float top[NT], sum[NT];
+    Softmax<NT, S> soft;
 #pragma unroll
-    for (int c = 0; c < NT; ++c) {
-        top[c] = kNone;
-        sum[c] = 0.f;
+    for (int c = 0; c < NT; ++c)
 #pragma unroll
         for (int s = 0; s < S; ++s) O[s][c] = floatx4{0, 0, 0, 0};
-    }
-    float unit = 0.f, per_unit = 1.f;                             // of the weights: a power of two near the largest s'
-    uint32_t limit2 = 0;                                          // kScaleSlack units as type t, twice
-    const uint32_t copy = (lane & 31) * 4;
+    const uint32_t copy = T::copy_of(lane);
     __syncthreads();
 
     for (int it = 0; it < steps; ++it) {
-        const int at = mine + it * W * kStep;
+        const int from = mine + it * W * kStep;
         if ((it + 1) % kPagesAhead == 0) ahead = pages_from(it + 1);
         const int l = 2 * ((it + 1) % kPagesAhead);
         // rows of the next step (after the last one: of the sequence's end, not used)
-        in.rows_of(row, at + W * kStep, __builtin_amdgcn_readlane(ahead, l), __builtin_amdgcn_readlane(ahead, l + 1));
+        in.rows_of(row, from + W * kStep, __builtin_amdgcn_readlane(ahead, l), __builtin_amdgcn_readlane(ahead, l + 1));
 
         floatx4 X[2][NT];
 #pragma unroll
@@ -266,88 +470,27 @@ __global__ __launch_bounds__(64 * (JOIN ? kJoinWaves : kOwnWaves), JOIN && NT ==
             for (int k = 0; k < ND; ++k) {
                 uintx4 op;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) op[j] = pair_of<0>(lds, f.k[u][k], j, copy);
+                for (int j = 0; j < 4; ++j) op[j] = T::pair<false>(lds, f.k[u][k], j, copy);
 #pragma unroll
                 for (int c = 0; c < NT; ++c) X[u][c] = mfma16<BF>(op, Q[c][k], X[u][c]);
             }
+        if constexpr (!JOIN) __builtin_amdgcn_sched_barrier(0);
         in.load_keys(f, row);
 
-        float vs[8], x[NT][8], peak[NT];
+        float ks[8], most = 0.f;
+        const uintx2 vs[2] = {f.vs[0], f.vs[1]};
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            vs[e] = scale_at<BF>(f.vs[e / 4], e & 3);
-#pragma unroll
-            for (int c = 0; c < NT; ++c) x[c][e] = X[e / 4][c][e & 3] * scale_at<BF>(f.ks[e / 4], e & 3);
+            ks[e] = scale_at<BF>(f.ks[e / 4], e & 3) * A.scale_log2;
+            most = fmaxf(most, scale_at<BF>(vs[e / 4], e & 3));
         }
-        if (at + kStep > whole_end || at < whole_from) {          // some row does not see all of these tokens
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int token = at + 4 * q + 16 * (e / 4) + (e & 3);
-                // A scale that is not finite reaches the rows that see it by way of their scores; where none does, or the tokens are
-                // past the end, it may be anything.
-                const bool bad = !(vs[e] <= 3.402823466e38f);
-#pragma unroll
-                for (int c = 0; c < NT; ++c)
-                    x[c][e] = token < see_lo[c] || token >= see_hi[c] ? -INFINITY : bad ? NAN : x[c][e];
-                if (bad || token < lo || token >= hi) vs[e] = 0.f;
-            }
-        }
-        // The largest scale of the values against the limit, two at a time as 16-bit integers (they are positive), and the scores
-        // against the maxima.
-        uint32_t most2 = limit2;
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) most2 = pk_max_u16(most2, f.vs[u][j]);
         in.load_scales(f, row);
-        bool move = most2 != limit2;
-#pragma unroll
-        for (int c = 0; c < NT; ++c) {
-            peak[c] = kNone;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) peak[c] = fmaxf(peak[c], x[c][e]);
-            move |= fmaf(peak[c], A.scale_log2, -top[c]) > kSlack;
-        }
-        if (__any(move)) {
-            float most = 0.f, ratio = 1.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) most = fmaxf(most, vs[e]);
-            most = fmaxf(most, __shfl_xor(most, 16));
-            most = fmaxf(most, __shfl_xor(most, 32));
-            if (most > kScaleSlack * unit) {                      // the same in all lanes
-                const float to = fminf(__uint_as_float(max(__float_as_uint(most) & 0x7f800000u, 0x00800000u)), 0x1p126f);
-                ratio = unit / to;
-                unit = to;
-                per_unit = 1.f / to;
-                limit2 = limit_of<BF>(unit);
-            }
-#pragma unroll
-            for (int c = 0; c < NT; ++c) {
-                float to = fmaxf(peak[c], __shfl_xor(peak[c], 16));
-                to = fmaxf(to, __shfl_xor(to, 32));
-                // (a column's maximum moves by its own scores alone: what other rows see has no part in its rounding)
-                to = fmaf(to, A.scale_log2, -top[c]) > kSlack ? to * A.scale_log2 : top[c];
-                const float shrink = exp2_fast(top[c] - to);
-                top[c] = to;
-                sum[c] *= shrink;
-#pragma unroll
-                for (int s = 0; s < S; ++s) O[s][c] *= shrink * ratio;
-            }
-        }
+        if constexpr (!JOIN) __builtin_amdgcn_sched_barrier(0);
         uintx4 w[NT];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) vs[e] *= per_unit;
-#pragma unroll
-        for (int c = 0; c < NT; ++c) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                x[c][e] = exp2_fast(fmaf(x[c][e], A.scale_log2, -top[c]));
-                sum[c] += x[c][e];
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) w[c][j] = pack_half2(x[c][2 * j] * vs[2 * j], x[c][2 * j + 1] * vs[2 * j + 1]);
-        }
+        soft.step(X, ks, [&](int e) { return scale_at<BF>(vs[e / 4], e & 3); }, most,
+                  from + kStep > whole_end || from < whole_from, seen, from + 4 * q, O, w);   // some row does not see all of these tokens
 
+        if constexpr (!JOIN) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int p = 0; p < P::count; ++p) {
             uint32_t pairs[4][2];                                 // [two tokens][half byte]
@@ -363,43 +506,66 @@ __global__ __launch_bounds__(64 * (JOIN ? kJoinWaves : kOwnWaves), JOIN && NT ==
                 for (int half = 0; half < 2; ++half) {
                     uintx4 op;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) op[j] = pair_of<128>(lds, pairs[j][half], i, copy);
+                    for (int j = 0; j < 4; ++j) op[j] = T::pair<true>(lds, pairs[j][half], i, copy);
                     const int s = 2 * (P::before(p) + i) + half;
 #pragma unroll
                     for (int c = 0; c < NT; ++c) O[s][c] = mfma16<false>(op, w[c], O[s][c]);
                 }
         }
+        if constexpr (!JOIN) __builtin_amdgcn_sched_barrier(0);
         in.load_values(f, row);
     }
 
+    soft.finish(O);
+    float (&top)[NT] = soft.top, (&sum)[NT] = soft.sum;
+
+    int last0 = row0;
+    __asm__("" : "+s"(last0));                                    // (places of the result are found now, not kept in registers all along)
+    if constexpr (!JOIN) {
 #pragma unroll
     for (int c = 0; c < NT; ++c) {
-        sum[c] += __shfl_xor(sum[c], 16);
-        sum[c] += __shfl_xor(sum[c], 32);
+        const int row = last0 + c * 16 + n, i = row / A.group, g = row - i * A.group;
+        if (row >= rows) continue;
+        const int64_t to = (int64_t)(q0 + i) * a.q_heads + h * A.group + g;
+        const float inv = inverse(soft.sum[c]);
+        // a piece's channels of one of O^T's rows lie side by side
 #pragma unroll
-        for (int s = 0; s < S; ++s) O[s][c] *= unit;
+        for (int p = 0; p < P::count; ++p)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                uint32_t o[P::width(0)];
+#pragma unroll
+                for (int j = 0; j < P::width(p); ++j) {
+                    const int s = 2 * (P::before(p) + j);
+                    o[j] = float_to_lp_any(O[s][c][r] * inv, BF) | (uint32_t)float_to_lp_any(O[s + 1][c][r] * inv, BF) << 16;
+                }
+                uint16_t* out = a.out + to * (32 * ND) + 2 * (16 * P::before(p) + (4 * q + r) * P::width(p));
+                if constexpr (P::width(0) == 4)
+                    if (P::width(p) == 4) *(uintx4*)out = uintx4{o[0], o[1], o[2], o[3]};
+                if constexpr (P::width(0) >= 2)
+                    if (P::width(p) == 2) *(uintx2*)out = uintx2{o[0], o[1]};
+                if (P::width(p) == 1) *(uint32_t*)out = o[0];
+            }
+        if (a.lse && q == 0) a.lse[to] = lse_of(soft.top[c], soft.sum[c]);
+    }
+        return;
     }
 
     const bool partial = A.splits > 1 && (hi - (lo & ~(kStep - 1))) > A.chunk;
     float* part = a.part + ((((int64_t)b * A.c.heads + h) * A.row_blocks + rb) * A.splits + split) * (R * (32 * ND + 2));
     auto finish = [&](int c, int s, floatx4 o, float t, float l) {
-        const int row = row0 + c * 16 + n, i = row / A.group, g = row - i * A.group;
+        const int row = last0 + c * 16 + n, i = row / A.group, g = row - i * A.group;
         if (row >= rows) return;
         const int64_t at = (int64_t)(q0 + i) * a.q_heads + h * A.group + g;
-        const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+        const float inv = inverse(l);
 #pragma unroll
         for (int r = 0; r < 4; ++r) a.out[at * (32 * ND) + channel_of<ND>(s, 4 * q + r)] = float_to_lp_any(o[r] * inv, BF);
-        if (a.lse && s == 0 && q == 0) a.lse[at] = l > 0.f || l != l ? (t + __log2f(l)) * 0.6931471805599453f : -INFINITY;
+        if (a.lse && s == 0 && q == 0) a.lse[at] = lse_of(t, l);
     };
 
-    if constexpr (!JOIN) {
-#pragma unroll
-        for (int c = 0; c < NT; ++c)
-#pragma unroll
-            for (int s = 0; s < S; ++s) finish(c, s, O[s][c], top[c], sum[c]);
-    } else {
+    if constexpr (JOIN) {
         // The waves' maxima and sums, then their products by way of the table's memory, a few subtiles at a time.
-        float* tops = (float*)(lds + kTableBytes);                // [waves][R]
+        float* tops = (float*)(lds + T::bytes);                // [waves][R]
         float* sums = tops + kJoinWaves * R;
         if (q == 0)
 #pragma unroll
@@ -419,7 +585,7 @@ __global__ __launch_bounds__(64 * (JOIN ? kJoinWaves : kOwnWaves), JOIN && NT ==
 #pragma unroll
             for (int s = 0; s < S; ++s) O[s][c] *= mine;
         }
-        constexpr int AT_ONCE = (int)(kTableBytes / 16) / (64 * kJoinWaves * NT);
+        constexpr int AT_ONCE = (int)(T::bytes / 16) / (64 * kJoinWaves * NT);
         static_assert(AT_ONCE >= 1, "the joined products fit the table's memory");
         floatx4* swap = (floatx4*)lds;                            // [waves][AT_ONCE][NT][64]
 #pragma unroll
@@ -441,7 +607,7 @@ __global__ __launch_bounds__(64 * (JOIN ? kJoinWaves : kOwnWaves), JOIN && NT ==
 #pragma unroll
                 for (int j = 1; j < NT; ++j) { tc = c == j ? t[j] : tc; lc = c == j ? l[j] : lc; }
                 if (partial) {
-                    if (row0 + c * 16 + n >= rows) continue;
+                    if (last0 + c * 16 + n >= rows) continue;
                     ((floatx4*)(part + 2 * R))[(s * NT + c) * 64 + lane] = o;
                     if (s == 0 && q == 0) {
                         part[c * 16 + n] = tc;
@@ -467,10 +633,8 @@ __global__ __launch_bounds__(kJoinThreads) void kv_join_kernel(AttendArgs A) {
     const int b = blockIdx.z, h = blockIdx.y, tile = blockIdx.x % (2 * ND * NT), rb = blockIdx.x / (2 * ND * NT);
     const int s = tile / NT, c = tile % NT;
     const int wave = threadIdx.x / 64, lane = threadIdx.x & 63, n = lane & 15, q = lane >> 4;
-    const int len = min(max(a.lens[b], 0), a.max_pages << A.c.page_shift);
-    const int q0 = a.q_start ? min(max(a.q_start[b], 0), (int)a.Tq) : b * a.max_q;
-    const int nq = a.q_start ? min(min(max(a.q_start[b + 1] - q0, 0), a.max_q), (int)a.Tq - q0) : a.max_q;
-    const int rows = nq * A.group, row0 = rb * R;
+    const Place place(a, A.c, A.group, b);
+    const int rows = place.rows, len = place.len, q0 = place.q0, nq = place.nq, row0 = rb * R;
     if (row0 + c * 16 >= rows) return;
     const int i0 = row0 / A.group, i1 = (min(row0 + R, rows) - 1) / A.group;
     const int hi = a.causal ? max(min(len, len - nq + i1 + 1), 0) : len;
@@ -523,24 +687,27 @@ __global__ __launch_bounds__(kJoinThreads) void kv_join_kernel(AttendArgs A) {
     for (int w = 1; w < WAVES; ++w) o += swap[w][lane];
     const int row = row0 + col, i = row / A.group, g = row - i * A.group;
     const int64_t at = (int64_t)(q0 + i) * a.q_heads + h * A.group + g;
-    const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+    const float inv = inverse(l);
 #pragma unroll
     for (int r = 0; r < 4; ++r) a.out[at * (32 * ND) + channel_of<ND>(s, 4 * q + r)] = float_to_lp_any(o[r] * inv, BF);
-    if (a.lse && s == 0 && q == 0) a.lse[at] = l > 0.f || l != l ? (t + __log2f(l)) * 0.6931471805599453f : -INFINITY;
+    if (a.lse && s == 0 && q == 0) a.lse[at] = lse_of(t, l);
 }
 
+// Tiles of a wave with rows of its own: as many as leave room for two waves a SIMD (O takes 8 registers a tile and 32 channels, q 4)
+static constexpr int own_tiles(int ND) { return ND <= 2 ? 4 : ND <= 4 ? 3 : ND <= 6 ? 2 : 1; }
+static constexpr int join_tiles(int ND) { return ND <= 2 ? 4 : ND <= 4 ? 3 : ND <= 6 ? 2 : 1; }
+
 KVPlan choose_kv_plan(const KVView& c, int q_heads, int B, int max_q, int64_t reach) {
-    const int group = q_heads / c.heads;
+    const int group = q_heads / c.heads, ND = c.d / 32;
     const int64_t rows = (int64_t)max_q * group;
-    const int most = c.d <= 128 ? 4 : 2;                         // tiles of a wave
     KVPlan p;
-    p.join = rows <= 16 * most || (int64_t)B * c.heads * cdiv(rows, 16 * most * kOwnWaves) < device_cu_count();
-    p.tiles = !p.join ? most : rows <= 16 ? 1 : rows <= 32 ? 2 : most;
+    p.join = rows <= 16 * join_tiles(ND) || (int64_t)B * c.heads * cdiv(rows, 16 * own_tiles(ND) * kOwnWaves) < device_cu_count();
+    p.tiles = !p.join ? own_tiles(ND) : (int)std::min(cdiv(rows, 16), (int64_t)join_tiles(ND));
     p.row_blocks = (int)cdiv(rows, 16 * p.tiles * (p.join ? 1 : kOwnWaves));
     p.splits = 1;
     p.chunk = INT32_MAX / 2;
     if (p.join) {
-        const int64_t wg = kJoinWaves * kStep, slots = (int64_t)device_cu_count() * 2, blocks = (int64_t)B * c.heads * p.row_blocks;
+        const int64_t wg = kJoinWaves * kStep, slots = (int64_t)device_cu_count(), blocks = (int64_t)B * c.heads * p.row_blocks;
         const int64_t want = blocks >= slots ? 1 : slots / blocks, steps = cdiv(reach, wg);
         p.splits = (int)std::min({want, steps, (int64_t)kMostSplits});
         if (p.splits > 1) p.chunk = cdiv(steps, p.splits) * wg;
@@ -548,12 +715,11 @@ KVPlan choose_kv_plan(const KVView& c, int q_heads, int B, int max_q, int64_t re
     return p;
 }
 
-template <bool BF, int ND, int NT, bool JOIN>
+template <bool BF, int ND, int NT>
 static fk_status launch_form(const AttendArgs& A, hipStream_t s) {
-    const int waves = JOIN ? kJoinWaves : kOwnWaves;
-    kv_attend_kernel<BF, ND, NT, JOIN><<<dim3(A.row_blocks * A.splits, A.c.heads, A.a.B), 64 * waves, 0, s>>>(A);
+    kv_attend_kernel<BF, ND, NT, true><<<dim3(A.row_blocks * A.splits, A.c.heads, A.a.B), 64 * kJoinWaves, 0, s>>>(A);
     FK_HIP(hipGetLastError());
-    if (JOIN && A.splits > 1) {
+    if (A.splits > 1) {
         kv_join_kernel<BF, ND, NT><<<dim3(A.row_blocks * 2 * ND * NT, A.c.heads, A.a.B), kJoinThreads, 0, s>>>(A);
         FK_HIP(hipGetLastError());
     }
@@ -562,12 +728,22 @@ static fk_status launch_form(const AttendArgs& A, hipStream_t s) {
 
 template <bool BF, int ND>
 static fk_status launch_width(const AttendArgs& A, const KVPlan& p, hipStream_t s) {
-    if (!p.join) return launch_form<BF, ND, (ND <= 4 ? 4 : 2), false>(A, s);
-    if (p.tiles == 1) return launch_form<BF, ND, 1, true>(A, s);
-    if (p.tiles == 2) return launch_form<BF, ND, 2, true>(A, s);
-    if constexpr (ND <= 4) return launch_form<BF, ND, 4, true>(A, s);
-    set_error("fk_kv_attend: no form of %d tiles for d=%d", p.tiles, 32 * ND);
-    return FK_EUNSUPPORTED;
+    if (!p.join) {
+        const int64_t blocks = (int64_t)A.row_blocks * A.c.heads * A.a.B;
+        if (blocks > INT32_MAX / 512) {
+            set_error("fk_kv_attend: unsupported size: %lld workgroups", (long long)blocks);
+            return FK_EUNSUPPORTED;
+        }
+        kv_attend_kernel<BF, ND, own_tiles(ND), false><<<(unsigned)blocks, 64 * kOwnWaves, 0, s>>>(A);
+        FK_HIP(hipGetLastError());
+        return FK_OK;
+    }
+    if (p.tiles == 1) return launch_form<BF, ND, 1>(A, s);
+    if constexpr (join_tiles(ND) >= 2)
+        if (p.tiles == 2) return launch_form<BF, ND, 2>(A, s);
+    if constexpr (join_tiles(ND) >= 3)
+        if (p.tiles == 3) return launch_form<BF, ND, 3>(A, s);
+    return launch_form<BF, ND, join_tiles(ND)>(A, s);
 }
 
 template <bool BF>
