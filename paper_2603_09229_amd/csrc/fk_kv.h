@@ -10,6 +10,16 @@ __device__ __forceinline__ uint16_t float_to_lp_any(float f, bool bf) {
     return bf ? __builtin_bit_cast(uint16_t, (__bf16)f) : __builtin_bit_cast(uint16_t, (_Float16)f);
 }
 
+// two of them in one register
+template <bool BF>
+__device__ __forceinline__ uint32_t pack_lp(float lo, float hi) {
+    typedef float float2v __attribute__((ext_vector_type(2)));
+    typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+    typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+    if constexpr (BF) return __builtin_bit_cast(uint32_t, __builtin_convertvector(float2v{lo, hi}, bf2));
+    else return __builtin_bit_cast(uint32_t, __builtin_convertvector(float2v{lo, hi}, half2v));
+}
+
 // Rows of type t at element strides.
 struct KVRows {
     const uint16_t* at;
