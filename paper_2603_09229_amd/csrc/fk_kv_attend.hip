@@ -220,11 +220,13 @@ struct Table {
         return *(const uint32_t*)(lds + at + (VALUES ? COPIES * 4 : 0));
     }
 
-    // Lanes 0..15 hold the keys' levels, lanes 16..31 the values'.
+    // The level that a lane brings to `fill`: lanes 0..15 the keys', lanes 16..31 the values'.
+    static __device__ __forceinline__ uint16_t level(const KVView& c, int h, int lane) {
+        return ((lane & 16) ? c.v_levels : c.k_levels)[h * 16 + (lane & 15)];
+    }
     template <bool BF, int THREADS>
-    static __device__ __forceinline__ void fill(uint8_t* lds, const KVView& c, int h, int lane) {
+    static __device__ __forceinline__ void fill(uint8_t* lds, uint16_t level, int lane) {
         constexpr int pieces = COPIES / 2, keys = pieces / 2;     // of 16 bytes: of a row, and of its keys' part
-        const uint16_t level = ((lane & 16) ? c.v_levels : c.k_levels)[h * 16 + (lane & 15)];
         const uint32_t mine = (lane & 16) ? float_to_half(lp_to_float(level, BF)) : level;
         const int side = lane & keys ? 16 : 0;
 #pragma unroll
@@ -405,6 +407,7 @@ void kv_attend_kernel(AttendArgs A) {
     const int split = JOIN ? blockIdx.x % A.splits : 0, rb = JOIN ? blockIdx.x / A.splits : A.row_blocks - 1 - blockIdx.x / blocks;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63, n = lane & 15, q = lane >> 4;
     const KVAttend& a = A.a;
+    const uint16_t level = T::level(A.c, h, lane);                // (the first load: the table waits for it alone)
 
     const Place at(a, A.c, A.group, b);
     const int rows = at.rows, len = at.len, q0 = at.q0, nq = at.nq, row0 = (JOIN ? rb : rb * kOwnWaves + wave) * R;
@@ -436,12 +439,12 @@ void kv_attend_kernel(AttendArgs A) {
         in.load_values(f, row);
     }
 
-    T::fill<BF, THREADS>(lds, A.c, h, lane);
     uintx4 Q[NT][ND];
     Seen<NT> seen;
     seen.lo = lo;
     seen.hi = hi;
     load_queries<ND, NT>(A, at, h, row0, n, q, Q, seen);
+    T::template fill<BF, THREADS>(lds, level, lane);
 
     floatx4 O[S][NT];
     Softmax<NT, S> soft;
@@ -621,14 +624,14 @@ void kv_attend_kernel(AttendArgs A) {
     }
 }
 
-// Joins the splits of one subtile of one row block.  All their maxima and sums are read at once, 16 columns by 32 splits, and become the
-// splits' factors in LDS; then each of the eight waves adds every eighth split's products, and the first wave what they have.
-constexpr int kJoinThreads = 512;
-template <bool BF, int ND, int NT>
-__global__ __launch_bounds__(kJoinThreads) void kv_join_kernel(AttendArgs A) {
-    constexpr int R = 16 * NT, WAVES = kJoinThreads / 64, LANES = kJoinThreads / 16;
+// Joins the splits of one subtile of one row block.  All their maxima and sums are read at once, 16 columns by 4 splits a wave, and become
+// the splits' factors in LDS; then each of the waves adds its share of the splits' products, and the first wave what they have.  Few
+// splits (many sequences) take one wave, many eight.
+template <bool BF, int ND, int NT, int WAVES, int MOST>
+__global__ __launch_bounds__(64 * WAVES) void kv_join_kernel(AttendArgs A) {
+    constexpr int R = 16 * NT, LANES = 4 * WAVES;
     __shared__ floatx4 swap[WAVES][64];
-    __shared__ float factor[kMostSplits][16], most[WAVES][16], all[WAVES][16];
+    __shared__ float factor[MOST][16], most[WAVES][16], all[WAVES][16];
     const KVAttend& a = A.a;
     const int b = blockIdx.z, h = blockIdx.y, tile = blockIdx.x % (2 * ND * NT), rb = blockIdx.x / (2 * ND * NT);
     const int s = tile / NT, c = tile % NT;
@@ -646,7 +649,7 @@ __global__ __launch_bounds__(kJoinThreads) void kv_join_kernel(AttendArgs A) {
     const int col = c * 16 + n;
     const bool live = row0 + col < rows;
 
-    constexpr int EACH = kMostSplits / LANES;
+    constexpr int EACH = MOST / LANES;
     float tops[EACH], sums[EACH], t = kNone, l = 0.f;
 #pragma unroll
     for (int k = 0; k < EACH; ++k) {
@@ -709,7 +712,10 @@ KVPlan choose_kv_plan(const KVView& c, int q_heads, int B, int max_q, int64_t re
     if (p.join) {
         const int64_t wg = kJoinWaves * kStep, slots = (int64_t)device_cu_count(), blocks = (int64_t)B * c.heads * p.row_blocks;
         const int64_t want = blocks >= slots ? 1 : slots / blocks, steps = cdiv(reach, wg);
+        // Splitting costs the second launch, about four steps of a workgroup: 8 heads of 128, one sequence of 700 tokens (3 steps) 10.6 us
+        // in one piece and 11.1 in three, of 1500 (6) 14.7 and 11.9 in six; 24 sequences of 2048 (8), 4 heads of 64, 13.5 and 13.9 in two.
         p.splits = (int)std::min({want, steps, (int64_t)kMostSplits});
+        if (steps - cdiv(steps, p.splits) <= 4) p.splits = 1;
         if (p.splits > 1) p.chunk = cdiv(steps, p.splits) * wg;
     }
     return p;
@@ -720,7 +726,9 @@ static fk_status launch_form(const AttendArgs& A, hipStream_t s) {
     kv_attend_kernel<BF, ND, NT, true><<<dim3(A.row_blocks * A.splits, A.c.heads, A.a.B), 64 * kJoinWaves, 0, s>>>(A);
     FK_HIP(hipGetLastError());
     if (A.splits > 1) {
-        kv_join_kernel<BF, ND, NT><<<dim3(A.row_blocks * 2 * ND * NT, A.c.heads, A.a.B), kJoinThreads, 0, s>>>(A);
+        const dim3 grid(A.row_blocks * 2 * ND * NT, A.c.heads, A.a.B);
+        if (A.splits <= 8) kv_join_kernel<BF, ND, NT, 1, 8><<<grid, 64, 0, s>>>(A);
+        else kv_join_kernel<BF, ND, NT, 8, kMostSplits><<<grid, 512, 0, s>>>(A);
         FK_HIP(hipGetLastError());
     }
     return FK_OK;
