@@ -63,10 +63,28 @@ __device__ __forceinline__ uint32_t limit_of(float unit) {
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// x / by for any x below 2^32: a multiplication by 2^(32 + s) / by, s = ceil(log2 by), less 2^32
+struct Divider {
+    int by;
+    uint32_t factor;
+    int shift1, shift2;
+    explicit Divider(int d) : by(d) {
+        int s = 0;
+        while (s < 31 && (1 << s) < d) ++s;
+        factor = (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << s) - d)) / d + 1);
+        shift1 = s ? 1 : 0;
+        shift2 = s ? s - 1 : 0;
+    }
+    __device__ __forceinline__ int quotient(int x) const {
+        const uint32_t t = __umulhi((uint32_t)x, factor);
+        return (int)((t + (((uint32_t)x - t) >> shift1)) >> shift2);
+    }
+};
+
 struct AttendArgs {
     KVView c;
     KVAttend a;
-    int group;                 // query heads to a cache head
+    Divider group;             // query heads to a cache head
     int splits, row_blocks;
     int chunk;
     float scale_log2;          // positive, so that scores that are not seen stay -inf:
@@ -130,10 +148,11 @@ template <bool BF, int ND>
 struct Reader {
     const AttendArgs& A;
     const int32_t* table;      // the sequence's pages
-    int h, last_half;          // cache head; start of the last 16 tokens that are read
+    int h, last_half;          // cache head; start of the last 16 tokens that the table has room for
     int lane, n, q;
 
-    // page of the 16 tokens from `at`, or of the last ones where that is past the end
+    // Page of the 16 tokens from `at`, or of the last ones that the table has room for.  Past the sequence's end its entries may be
+    // anything; what is read by them lies in the cache and is not used.
     __device__ __forceinline__ int page_of(int at) const {
         const int p = table[min(at, last_half) >> A.c.page_shift];
         return min(max(p, 0), (int)A.c.pages - 1);
@@ -229,7 +248,7 @@ struct Table {
         constexpr int pieces = COPIES / 2, keys = pieces / 2;     // of 16 bytes: of a row, and of its keys' part
         const uint32_t mine = (lane & 16) ? float_to_half(lp_to_float(level, BF)) : level;
         const int side = lane & keys ? 16 : 0;
-#pragma unroll
+#pragma unroll 2
         for (int i = 0; i < bytes / 16 / THREADS; ++i) {
             const int at = i * THREADS + threadIdx.x, code = at / pieces;
             const uint32_t pair = (uint32_t)__shfl((int)mine, side + (code & 15)) | ((uint32_t)__shfl((int)mine, side + (code >> 4)) << 16);
@@ -263,9 +282,9 @@ __device__ __forceinline__ void load_queries(const AttendArgs& A, const Place& p
     const KVAttend& a = A.a;
 #pragma unroll
     for (int c = 0; c < NT; ++c) {
-        const int row = row0 + c * 16 + n, i = row / A.group, g = row - i * A.group;
+        const int row = row0 + c * 16 + n, i = A.group.quotient(row), g = row - i * A.group.by;
         const bool live = row < p.rows;
-        const uint16_t* at = a.q.at + (int64_t)(p.q0 + i) * a.q.token + (int64_t)(h * A.group + g) * a.q.head + q * (8 * ND);
+        const uint16_t* at = a.q.at + (int64_t)(p.q0 + i) * a.q.token + (int64_t)(h * A.group.by + g) * a.q.head + q * (8 * ND);
 #pragma unroll
         for (int k = 0; k < ND; ++k) {
             Q[c][k] = uintx4{0, 0, 0, 0};
@@ -409,12 +428,27 @@ void kv_attend_kernel(AttendArgs A) {
     const KVAttend& a = A.a;
     const uint16_t level = T::level(A.c, h, lane);                // (the first load: the table waits for it alone)
 
-    const Place at(a, A.c, A.group, b);
+    // Without a window the first step does not depend on the sequence's length, and its loads are issued before that is known.
+    Reader<BF, ND> in{A, a.pages + (int64_t)b * a.max_pages, h, (a.max_pages << A.c.page_shift) - 16, lane, n, q};
+    int ahead = 0, mine = JOIN ? split * A.chunk + wave * kStep : 0;   // lane l: page of half l % 2 of step l / 2 of this batch; first step
+    auto pages_from = [&](int step) { return in.page_of(mine + (step + lane / 2) * W * kStep + (lane & 1) * 16); };
+    Codes<ND> f;                                                  // the step's, refilled piece by piece as it is used up
+    int64_t row[2];
+    auto begin = [&] {
+        ahead = pages_from(0);
+        in.rows_of(row, mine, __builtin_amdgcn_readlane(ahead, 0), __builtin_amdgcn_readlane(ahead, 1));
+        in.load_keys(f, row);
+        in.load_scales(f, row);
+        in.load_values(f, row);
+    };
+    if (!a.window) begin();
+
+    const Place at(a, A.c, A.group.by, b);
     const int rows = at.rows, len = at.len, q0 = at.q0, nq = at.nq, row0 = (JOIN ? rb : rb * kOwnWaves + wave) * R;
     if ((JOIN ? row0 : rb * kOwnWaves * R) >= rows) return;       // the whole workgroup
 
     // tokens that the wave's rows see
-    const int i0 = row0 / A.group, i1 = (min(row0 + R, rows) - 1) / A.group;
+    const int i0 = A.group.quotient(row0), i1 = A.group.quotient(max(min(row0 + R, rows) - 1, 0));
     const int p0 = len - nq + i0, p1 = len - nq + i1;
     const int hi = row0 >= rows ? 0 : a.causal ? max(min(len, p1 + 1), 0) : len;
     const int lo = a.window ? max(0, p0 - a.window + 1) : 0;
@@ -423,21 +457,9 @@ void kv_attend_kernel(AttendArgs A) {
     if (JOIN && split > 0 && first >= hi) return;                 // the whole workgroup
     // a step is whole where every row sees all of its tokens
     const int whole_end = a.causal ? min(len, p0 + 1) : len, whole_from = a.window ? p1 - a.window + 1 : 0;
-    const int mine = first + (JOIN ? wave * kStep : 0);
+    mine = first + (JOIN ? wave * kStep : 0);
     const int steps = end > mine ? (end - mine + W * kStep - 1) / (W * kStep) : 0;
-
-    Reader<BF, ND> in{A, a.pages + (int64_t)b * a.max_pages, h, max(hi - 1, 0) & ~15, lane, n, q};
-    int ahead = 0;                                                // lane l: page of half l % 2 of step l / 2 of this batch
-    auto pages_from = [&](int step) { return in.page_of(mine + (step + lane / 2) * W * kStep + (lane & 1) * 16); };
-    Codes<ND> f;                                                  // the step's, refilled piece by piece as it is used up
-    int64_t row[2];
-    if (steps) {
-        ahead = pages_from(0);
-        in.rows_of(row, mine, __builtin_amdgcn_readlane(ahead, 0), __builtin_amdgcn_readlane(ahead, 1));
-        in.load_keys(f, row);
-        in.load_scales(f, row);
-        in.load_values(f, row);
-    }
+    if (a.window && steps) begin();
 
     uintx4 Q[NT][ND];
     Seen<NT> seen;
@@ -527,9 +549,9 @@ void kv_attend_kernel(AttendArgs A) {
     if constexpr (!JOIN) {
 #pragma unroll
     for (int c = 0; c < NT; ++c) {
-        const int row = last0 + c * 16 + n, i = row / A.group, g = row - i * A.group;
+        const int row = last0 + c * 16 + n, i = A.group.quotient(row), g = row - i * A.group.by;
         if (row >= rows) continue;
-        const int64_t to = (int64_t)(q0 + i) * a.q_heads + h * A.group + g;
+        const int64_t to = (int64_t)(q0 + i) * a.q_heads + h * A.group.by + g;
         const float inv = inverse(soft.sum[c]);
         // a piece's channels of one of O^T's rows lie side by side
 #pragma unroll
@@ -557,9 +579,9 @@ void kv_attend_kernel(AttendArgs A) {
     const bool partial = A.splits > 1 && (hi - (lo & ~(kStep - 1))) > A.chunk;
     float* part = a.part + ((((int64_t)b * A.c.heads + h) * A.row_blocks + rb) * A.splits + split) * (R * (32 * ND + 2));
     auto finish = [&](int c, int s, floatx4 o, float t, float l) {
-        const int row = last0 + c * 16 + n, i = row / A.group, g = row - i * A.group;
+        const int row = last0 + c * 16 + n, i = A.group.quotient(row), g = row - i * A.group.by;
         if (row >= rows) return;
-        const int64_t at = (int64_t)(q0 + i) * a.q_heads + h * A.group + g;
+        const int64_t at = (int64_t)(q0 + i) * a.q_heads + h * A.group.by + g;
         const float inv = inverse(l);
 #pragma unroll
         for (int r = 0; r < 4; ++r) a.out[at * (32 * ND) + channel_of<ND>(s, 4 * q + r)] = float_to_lp_any(o[r] * inv, BF);
@@ -568,23 +590,20 @@ void kv_attend_kernel(AttendArgs A) {
 
     if constexpr (JOIN) {
         // The waves' maxima and sums, then their products by way of the table's memory, a few subtiles at a time.
-        float* tops = (float*)(lds + T::bytes);                // [waves][R]
-        float* sums = tops + kJoinWaves * R;
+        static_assert(kJoinWaves == 8, "eight of them, two pieces of 16 bytes");
+        floatx4* tops = (floatx4*)(lds + T::bytes);               // [R][waves]
+        floatx4* sums = tops + R * 2;
         if (q == 0)
 #pragma unroll
-            for (int c = 0; c < NT; ++c) {
-                tops[wave * R + c * 16 + n] = sum[c] == 0.f ? kNone : top[c];
-                sums[wave * R + c * 16 + n] = sum[c];
-            }
+            for (int c = 0; c < NT; ++c) ((float*)(tops + (c * 16 + n) * 2))[wave] = sum[c] == 0.f ? kNone : top[c];
         __syncthreads();                                          // the table is done with, too
-        float t[NT], l[NT];
+        float t[NT];
 #pragma unroll
         for (int c = 0; c < NT; ++c) {
-            t[c] = kNone;
-            l[c] = 0.f;
-            for (int w = 0; w < kJoinWaves; ++w) t[c] = fmaxf(t[c], tops[w * R + c * 16 + n]);
-            for (int w = 0; w < kJoinWaves; ++w) l[c] += sums[w * R + c * 16 + n] * exp2_fast(tops[w * R + c * 16 + n] - t[c]);
+            const floatx4 u = tops[(c * 16 + n) * 2], v = tops[(c * 16 + n) * 2 + 1];
+            t[c] = fmaxf(fmaxf(fmaxf(u[0], u[1]), fmaxf(u[2], u[3])), fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])));
             const float mine = sum[c] == 0.f ? 0.f : exp2_fast(top[c] - t[c]);
+            if (q == 0) ((float*)(sums + (c * 16 + n) * 2))[wave] = sum[c] * mine;
 #pragma unroll
             for (int s = 0; s < S; ++s) O[s][c] *= mine;
         }
@@ -606,9 +625,11 @@ void kv_attend_kernel(AttendArgs A) {
                 floatx4 o = {0, 0, 0, 0};
 #pragma unroll
                 for (int w = 0; w < kJoinWaves; ++w) o += swap[(w * AT_ONCE * NT + i) * 64 + lane];
-                float tc = t[0], lc = l[0];
+                const floatx4 l4 = sums[(c * 16 + n) * 2] + sums[(c * 16 + n) * 2 + 1];
+                const float lc = (l4[0] + l4[1]) + (l4[2] + l4[3]);
+                float tc = t[0];
 #pragma unroll
-                for (int j = 1; j < NT; ++j) { tc = c == j ? t[j] : tc; lc = c == j ? l[j] : lc; }
+                for (int j = 1; j < NT; ++j) tc = c == j ? t[j] : tc;
                 if (partial) {
                     if (last0 + c * 16 + n >= rows) continue;
                     ((floatx4*)(part + 2 * R))[(s * NT + c) * 64 + lane] = o;
@@ -636,10 +657,10 @@ __global__ __launch_bounds__(64 * WAVES) void kv_join_kernel(AttendArgs A) {
     const int b = blockIdx.z, h = blockIdx.y, tile = blockIdx.x % (2 * ND * NT), rb = blockIdx.x / (2 * ND * NT);
     const int s = tile / NT, c = tile % NT;
     const int wave = threadIdx.x / 64, lane = threadIdx.x & 63, n = lane & 15, q = lane >> 4;
-    const Place place(a, A.c, A.group, b);
+    const Place place(a, A.c, A.group.by, b);
     const int rows = place.rows, len = place.len, q0 = place.q0, nq = place.nq, row0 = rb * R;
     if (row0 + c * 16 >= rows) return;
-    const int i0 = row0 / A.group, i1 = (min(row0 + R, rows) - 1) / A.group;
+    const int i0 = A.group.quotient(row0), i1 = A.group.quotient(max(min(row0 + R, rows) - 1, 0));
     const int hi = a.causal ? max(min(len, len - nq + i1 + 1), 0) : len;
     const int lo = (a.window ? max(0, len - nq + i0 - a.window + 1) : 0) & ~(kStep - 1);
     if (hi - lo <= A.chunk) return;                               // one split has written the result itself
@@ -688,8 +709,8 @@ __global__ __launch_bounds__(64 * WAVES) void kv_join_kernel(AttendArgs A) {
     for (int w = 0; w < WAVES; ++w) l += all[w][n];
 #pragma unroll
     for (int w = 1; w < WAVES; ++w) o += swap[w][lane];
-    const int row = row0 + col, i = row / A.group, g = row - i * A.group;
-    const int64_t at = (int64_t)(q0 + i) * a.q_heads + h * A.group + g;
+    const int row = row0 + col, i = A.group.quotient(row), g = row - i * A.group.by;
+    const int64_t at = (int64_t)(q0 + i) * a.q_heads + h * A.group.by + g;
     const float inv = inverse(l);
 #pragma unroll
     for (int r = 0; r < 4; ++r) a.out[at * (32 * ND) + channel_of<ND>(s, 4 * q + r)] = float_to_lp_any(o[r] * inv, BF);
@@ -769,7 +790,7 @@ static fk_status launch_type(const AttendArgs& A, const KVPlan& p, hipStream_t s
 }
 
 fk_status launch_kv_attend(const KVView& c, const KVAttend& a, const KVPlan& p, hipStream_t s) {
-    const AttendArgs A{c, a, a.q_heads / c.heads, p.splits, p.row_blocks, (int)p.chunk, fmaxf(fabsf(a.scale) * 1.44269504088896341f, 1e-37f), a.scale < 0.f ? 0x80008000u : 0u};
+    const AttendArgs A{c, a, Divider(a.q_heads / c.heads), p.splits, p.row_blocks, (int)p.chunk, fmaxf(fabsf(a.scale) * 1.44269504088896341f, 1e-37f), a.scale < 0.f ? 0x80008000u : 0u};
     return c.bf ? launch_type<true>(A, p, s) : launch_type<false>(A, p, s);
 }
 
