@@ -394,7 +394,7 @@ def fk_kv_read(cache: KVCache, slots, *, k_out=None, v_out=None):
     if k_out is None:
         k_out = torch.empty(shape, dtype=cache.dtype, device=cache.device)
     if v_out is None:
-        v_out = torch.empty(shape, dtype=cache.dtype, device=cache.device)
+        v_out = torch.empty_like(k_out)
     _check(lib().fk_kv_read(cache._ref, _array(slots, "slots", cache, torch.int64, (T,)), T,
                             _array(k_out, "k_out", cache, cache.dtype, shape), _array(v_out, "v_out", cache, cache.dtype, shape),
                             _raw_stream(cache)))

@@ -45,8 +45,13 @@ __device__ __forceinline__ floatx4 mfma16(uintx4 a, uintx4 b, floatx4 c) {
 }
 
 __device__ __forceinline__ uint32_t float_to_half(float f) { return __builtin_bit_cast(uint16_t, (_Float16)f); }
-__device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
-    return float_to_half(lo) | float_to_half(hi) << 16;
+// two products rounded to fp16, each by the instruction that multiplies
+__device__ __forceinline__ uint32_t pack_products(float a, float b, float c, float d) {
+    typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+    half2v r;
+    r[0] = (_Float16)(a * b);
+    r[1] = (_Float16)(c * d);
+    return __builtin_bit_cast(uint32_t, r);
 }
 
 __device__ __forceinline__ uint32_t pk_max_u16(uint32_t a, uint32_t b) {
@@ -134,9 +139,9 @@ __device__ __forceinline__ float lane_of(float v, int lane) { return __int_as_fl
 // addition each.
 typedef __attribute__((address_space(1))) const uint8_t* Base;
 __device__ __forceinline__ Base base_of(const void* p, int64_t bytes) {
-    const uint64_t v = (uint64_t)p + bytes;
-    const uint32_t lo = __builtin_amdgcn_readfirstlane((int)(uint32_t)v), hi = __builtin_amdgcn_readfirstlane((int)(uint32_t)(v >> 32));
-    return (Base)((uint64_t)hi << 32 | lo);
+    uint64_t v = (uint64_t)p + bytes;
+    __asm__("" : "+s"(v));                                        // (or the compiler adds the lane's offset to p outside the loop)
+    return (Base)v;
 }
 template <class T>
 __device__ __forceinline__ T load_at(Base base, uint32_t offset) {
@@ -306,73 +311,77 @@ __device__ __forceinline__ float lse_of(float top, float sum) {
 template <int NT, int S>
 struct Softmax {
     float top[NT], sum[NT];    // reference of the exponents (0 before anything is seen), sum of the exponentials
+    float bar[NT];             // a score this much above the reference moves it: any before the first, then kSlack
     float unit = 0.f, per_unit = 1.f;
-    float limit = 0.f;         // kScaleSlack units
+    uint32_t limit2 = 0;       // kScaleSlack units as two numbers of type t
 
     __device__ __forceinline__ Softmax() {
 #pragma unroll
-        for (int c = 0; c < NT; ++c) top[c] = sum[c] = 0.f;
+        for (int c = 0; c < NT; ++c) {
+            top[c] = sum[c] = 0.f;
+            bar[c] = kNone;
+        }
     }
 
     // One step's scores X (before the keys' scales ks, which come times scale log2 e) become weights w; products O move with their
-    // reference.  The lane's e-th score is of token first + 16 (e / 4) + e % 4, scale_of(e) its values' scale and most the largest of
-    // the step where every row sees all of it.
-    template <class ScaleOf>
-    __device__ __forceinline__ void step(const floatx4 (&X)[2][NT], const float (&ks)[8], ScaleOf scale_of, float most, bool masked,
+    // reference.  The lane's e-th score is of token first + 16 (e / 4) + e % 4, vs has its values' scales, 16 bits
+    // each, and loses those that must not be multiplied.
+    template <bool BF>
+    __device__ __forceinline__ void step(const floatx4 (&X)[2][NT], const float (&ks)[8], uintx2 (&vs)[2], bool masked,
                                          const Seen<NT>& seen, int first, floatx4 (&O)[S][NT], uintx4 (&w)[NT]) {
         float x[NT][8], peak[NT];
-        uint32_t dead = 0;                                        // bit e: a scale that must not be multiplied
 #pragma unroll
         for (int c = 0; c < NT; ++c)
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[c][e] = fmaf(X[e / 4][c][e & 3], ks[e], -top[c]);
         if (masked) {
-            most = 0.f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const int token = first + 16 * (e / 4) + (e & 3);
                 // A scale that is not finite reaches the rows that see it by way of their scores; where none does, or the tokens are
                 // past the end, it may be anything.
-                const float v = scale_of(e);
+                const float v = scale_at<BF>(vs[e / 4], e & 3);
                 const bool bad = !(v <= 3.402823466e38f), out = bad || token < seen.lo || token >= seen.hi;
 #pragma unroll
                 for (int c = 0; c < NT; ++c)
                     x[c][e] = token >= seen.hi || token - seen.pos[c] > seen.after || token - seen.pos[c] <= seen.before ? -INFINITY
                             : bad ? NAN : x[c][e];
-                dead |= out ? 1u << e : 0u;
-                most = fmaxf(most, out ? 0.f : v);
+                vs[e / 4][(e & 3) / 2] &= out ? (e & 1 ? 0x0000ffffu : 0xffff0000u) : 0xffffffffu;
             }
         }
-        bool move = most > limit;
+        // The scales against the limit, two at a time as 16-bit integers (they are positive)
+        const uint32_t most2 = pk_max_u16(pk_max_u16(vs[0][0], vs[0][1]), pk_max_u16(vs[1][0], vs[1][1]));
+        bool move = pk_max_u16(most2, limit2) != limit2;
 #pragma unroll
         for (int c = 0; c < NT; ++c) {
             peak[c] = x[c][0];
 #pragma unroll
             for (int e = 1; e < 8; ++e) peak[c] = fmaxf(peak[c], x[c][e]);
-            move |= peak[c] > (sum[c] == 0.f ? -3.402823466e38f : kSlack);
+            move |= peak[c] > bar[c];
         }
         if (__any(move)) {
-            float ratio = 1.f;
+            float ratio = 1.f, most = fmaxf(lp_to_float((uint16_t)most2, BF), lp_to_float((uint16_t)(most2 >> 16), BF));
             most = fmaxf(most, __shfl_xor(most, 16));
             most = fmaxf(most, __shfl_xor(most, 32));
-            if (most > limit) {                                   // the same in all lanes
+            if (most > kScaleSlack * unit) {                      // the same in all lanes
                 const float to = fminf(__uint_as_float(max(__float_as_uint(most) & 0x7f800000u, 0x00800000u)), 0x1p126f);
                 ratio = unit / to;
                 unit = to;
                 per_unit = 1.f / to;
-                limit = fminf(kScaleSlack * to, 3.402823466e38f);
+                limit2 = limit_of<BF>(to);
             }
 #pragma unroll
             for (int c = 0; c < NT; ++c) {
                 // (a column's reference moves by its own scores alone: what other rows see has no part in its rounding)
-                float by = fmaxf(peak[c], __shfl_xor(peak[c], 16)), had = sum[c] + __shfl_xor(sum[c], 16);
+                float by = fmaxf(peak[c], __shfl_xor(peak[c], 16));
                 by = fmaxf(by, __shfl_xor(by, 32));
-                had += __shfl_xor(had, 32);
-                by = by > (had == 0.f ? -3.402823466e38f : kSlack) ? by : 0.f;
-                const float shrink = exp2_fast(-by);
+                const bool moves = by > bar[c];
+                by = moves ? by : 0.f;
+                // before anything is seen sum and products are zero, and the first reference may lie anywhere
+                const float shrink = bar[c] == kNone ? 0.f : exp2_fast(-by), f = shrink * ratio;
+                bar[c] = moves ? kSlack : bar[c];
                 top[c] += by;
-                if (had != 0.f) sum[c] *= shrink;
-                const float f = had != 0.f ? shrink * ratio : 0.f;
+                sum[c] *= shrink;
 #pragma unroll
                 for (int s = 0; s < S; ++s) O[s][c] *= f;
 #pragma unroll
@@ -381,11 +390,7 @@ struct Softmax {
         }
         float v[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = scale_of(e) * per_unit;
-        if (masked) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = dead >> e & 1 ? 0.f : v[e];
-        }
+        for (int e = 0; e < 8; ++e) v[e] = scale_at<BF>(vs[e / 4], e & 3) * per_unit;
 #pragma unroll
         for (int c = 0; c < NT; ++c) {
 #pragma unroll
@@ -394,7 +399,7 @@ struct Softmax {
                 sum[c] += x[c][e];
             }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) w[c][j] = pack_half2(x[c][2 * j] * v[2 * j], x[c][2 * j + 1] * v[2 * j + 1]);
+            for (int j = 0; j < 4; ++j) w[c][j] = pack_products(x[c][2 * j], v[2 * j], x[c][2 * j + 1], v[2 * j + 1]);
         }
     }
 
@@ -502,18 +507,15 @@ void kv_attend_kernel(AttendArgs A) {
         if constexpr (!JOIN) __builtin_amdgcn_sched_barrier(0);
         in.load_keys(f, row);
 
-        float ks[8], most = 0.f;
-        const uintx2 vs[2] = {f.vs[0], f.vs[1]};
+        float ks[8];
+        uintx2 vs[2] = {f.vs[0], f.vs[1]};
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            ks[e] = scale_at<BF>(f.ks[e / 4], e & 3) * A.scale_log2;
-            most = fmaxf(most, scale_at<BF>(vs[e / 4], e & 3));
-        }
+        for (int e = 0; e < 8; ++e) ks[e] = scale_at<BF>(f.ks[e / 4], e & 3) * A.scale_log2;
         in.load_scales(f, row);
         if constexpr (!JOIN) __builtin_amdgcn_sched_barrier(0);
         uintx4 w[NT];
-        soft.step(X, ks, [&](int e) { return scale_at<BF>(vs[e / 4], e & 3); }, most,
-                  from + kStep > whole_end || from < whole_from, seen, from + 4 * q, O, w);   // some row does not see all of these tokens
+        soft.template step<BF>(X, ks, vs, from + kStep > whole_end || from < whole_from,   // some row does not see all of these tokens
+                               seen, from + 4 * q, O, w);
 
         if constexpr (!JOIN) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
