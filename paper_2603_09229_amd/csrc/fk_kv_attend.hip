@@ -19,7 +19,16 @@
 // are multiplied as fp16 whatever t is (levels are at most 1 or so, 11 bits hold a bf16's 8).
 //
 // The running maximum is only moved when a score passes it by 2^kSlack, the weights' scale (a power of two near the largest s') when one
-// passes that by 2^kScaleSlack: the sums are then multiplied once.  Weights stay below 2^15 and fit fp16.
+// passes that by 2^kScaleSlack: the sums are then multiplied once.  Weights stay below 2^15 and fit fp16; relative to their scale they keep
+// 11 bits, as many as the values have in an uncoded cache of fp16, and sums and statistics are fp32.
+//
+// What bounds it.  Single tokens (at most 16 query rows to a cache head): bytes, 2 (d/2 + 2) a token and head.  64 sequences of up to 8192
+// tokens, 8 heads of 128: 353 MB in 81 us, 4.3 TB/s (5.0 where they are equally long; a large copy reaches 5.2); one of 131072: 138 MB in 31 us
+// and the join 5.  Few tokens: a workgroup's fixed cost, about 6 us with its launch, of which the chain of first loads (page, codes; not the length, see
+// below), the table (64 KiB of LDS) and the exchange between the waves are a third each, then 1.1 us a step of 8 x 32 tokens.
+// Many rows: vector instructions.  A step of 48 rows and 32 tokens at d = 128 takes 48 MFMA (768 cycles), 64 lookups and about 240 vector
+// instructions with 24 exponentials (1340 cycles); two waves a SIMD overlap a third of the two.  Two sequences of 4096 queries over up to
+// 9000 tokens, 32 query heads: 852 GFLOP in 1042 us, 0.82 PFLOP/s; a large product of the library reaches 1.2 on this card.
 #include <algorithm>
 
 #include "fk_device.h"
@@ -719,7 +728,9 @@ __global__ __launch_bounds__(64 * WAVES) void kv_join_kernel(AttendArgs A) {
     if (a.lse && s == 0 && q == 0) a.lse[at] = lse_of(t, l);
 }
 
-// Tiles of a wave with rows of its own: as many as leave room for two waves a SIMD (O takes 8 registers a tile and 32 channels, q 4)
+// Most tiles of a wave: as many as leave room for two waves a SIMD without spills (O takes 8 registers a tile and 32 channels, q 4).  With
+// one more, 2 sequences of 1024 queries over 4096 tokens, 16 query heads: d = 256 two tiles 495 us, one 232; d = 224 395 and 226.  With
+// one less: d = 128 chunk as above two tiles 1245 us, three 1220, when they were measured.
 static constexpr int own_tiles(int ND) { return ND <= 2 ? 4 : ND <= 4 ? 3 : ND <= 6 ? 2 : 1; }
 static constexpr int join_tiles(int ND) { return ND <= 2 ? 4 : ND <= 4 ? 3 : ND <= 6 ? 2 : 1; }
 
@@ -727,12 +738,15 @@ KVPlan choose_kv_plan(const KVView& c, int q_heads, int B, int max_q, int64_t re
     const int group = q_heads / c.heads, ND = c.d / 32;
     const int64_t rows = (int64_t)max_q * group;
     KVPlan p;
+    // Waves with rows of their own need no exchange at the end, but the rows' workgroups alone have to fill the chip (8 x 5 queries of 16
+    // heads of 256 over 4000 tokens: 16 workgroups 360 us, divided by tokens too 22); otherwise the tokens are divided.
     p.join = rows <= 16 * join_tiles(ND) || (int64_t)B * c.heads * cdiv(rows, 16 * own_tiles(ND) * kOwnWaves) < device_cu_count();
     p.tiles = !p.join ? own_tiles(ND) : (int)std::min(cdiv(rows, 16), (int64_t)join_tiles(ND));
     p.row_blocks = (int)cdiv(rows, 16 * p.tiles * (p.join ? 1 : kOwnWaves));
     p.splits = 1;
     p.chunk = INT32_MAX / 2;
     if (p.join) {
+        // One workgroup to a compute unit: 8 heads, one sequence of 131072 tokens 64 splits 40.6 us, 32 37.8, 24 43.7.
         const int64_t wg = kJoinWaves * kStep, slots = (int64_t)device_cu_count(), blocks = (int64_t)B * c.heads * p.row_blocks;
         const int64_t want = blocks >= slots ? 1 : slots / blocks, steps = cdiv(reach, wg);
         // Splitting costs the second launch, about four steps of a workgroup: 8 heads of 128, one sequence of 700 tokens (3 steps) 10.6 us

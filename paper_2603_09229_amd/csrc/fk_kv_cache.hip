@@ -6,6 +6,9 @@
 // magnitude is found on the 16 bits themselves: without the sign they order as integers, values that are not finite last.
 //
 // A row is held by L lanes of a wave, 8 channels (16 bytes) each, so that rows of 64 / L heads move together.
+//
+// What bounds it: bytes for many tokens (16384 of 8 + 8 + 32 rows of 128: 361 MB in 76 us, 4.7 TB/s, where a large copy reaches 5.2; reading
+// 20000 tokens of 8 + 8 rows of 128: 103 MB in 24 us, 4.3), the launch and three dependent loads for few (3.9 and 2.1 us for one token).
 #include "fk_device.h"
 #include "fk_kv.h"
 
