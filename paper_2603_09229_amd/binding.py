@@ -355,6 +355,16 @@ def _array(t: torch.Tensor, name: str, cache: KVCache, dtype, shape) -> int:
     return _dev(t, name, dtype, shape).data_ptr()
 
 
+def _result(t, name: str, cache: KVCache, like: torch.Tensor, shape):
+    """The caller's tensor for a result, or a new one with the rows of `like` -> (tensor, pointer)."""
+    if t is not None:
+        return t, _array(t, name, cache, cache.dtype, shape)
+    t = torch.empty_like(like)                   # (half a microsecond less than torch.empty with a type and a device)
+    if not t.is_contiguous():
+        t = torch.empty(shape, dtype=cache.dtype, device=cache.device)
+    return t, t.data_ptr()
+
+
 def _raw_stream(cache: KVCache) -> int:
     return torch._C._cuda_getCurrentRawStream(cache._index)
 
@@ -379,9 +389,7 @@ def fk_kv_append(cache: KVCache, k, v, slots, *, positions=None, cos_sin=None, i
     if q is not None:
         heads = q.shape[1]
         qp, qt, qh = _rows(q, "q", cache, T, heads)
-        if q_out is None:
-            q_out = torch.empty((T, heads, d), dtype=cache.dtype, device=cache.device)
-        qo = _array(q_out, "q_out", cache, cache.dtype, (T, heads, d))
+        q_out, qo = _result(q_out, "q_out", cache, q, (T, heads, d))
     _check(lib().fk_kv_append(cache._ref, kp, kt, kh, vp, vt, vh, _array(slots, "slots", cache, torch.int64, (T,)), T, cs, ps,
                               max_pos, rot, interleaved, qp, qt, qh, heads, qo, _raw_stream(cache)))
     return q_out if q is not None else None
@@ -392,12 +400,12 @@ def fk_kv_read(cache: KVCache, slots, *, k_out=None, v_out=None):
     T = slots.shape[0]
     shape = (T, cache.heads, cache.d)
     if k_out is None:
-        k_out = torch.empty(shape, dtype=cache.dtype, device=cache.device)
-    if v_out is None:
-        v_out = torch.empty_like(k_out)
-    _check(lib().fk_kv_read(cache._ref, _array(slots, "slots", cache, torch.int64, (T,)), T,
-                            _array(k_out, "k_out", cache, cache.dtype, shape), _array(v_out, "v_out", cache, cache.dtype, shape),
-                            _raw_stream(cache)))
+        k_out = cache.k_scale.new_empty(shape)
+        kp = k_out.data_ptr()
+    else:
+        kp = _array(k_out, "k_out", cache, cache.dtype, shape)
+    v_out, vp = _result(v_out, "v_out", cache, k_out, shape)
+    _check(lib().fk_kv_read(cache._ref, _array(slots, "slots", cache, torch.int64, (T,)), T, kp, vp, _raw_stream(cache)))
     return k_out, v_out
 
 
@@ -431,12 +439,11 @@ def fk_kv_attend(cache: KVCache, q, pages, lens, *, q_start=None, max_q=None, ma
         max_len = max_pages * cache.page_size
     if ws is None:
         ws = make_kv_workspace(cache, B, heads, Tq, max_q, max_len)
-    if out is None:
-        out = torch.empty((Tq, heads, cache.d), dtype=cache.dtype, device=cache.device)
+    out, op = _result(out, "out", cache, q, (Tq, heads, cache.d))
     le = torch.empty((Tq, heads), dtype=torch.float32, device=cache.device) if lse else None
     _check(lib().fk_kv_attend(cache._ref, qp, qt, qh, heads, Tq, _array(pages, "pages", cache, torch.int32, (B, max_pages)), max_pages,
                               _array(lens, "lens", cache, torch.int32, (B,)), qs, B, max_q, max_len,
                               cache.d ** -0.5 if scale is None else scale, causal, window,
-                              _array(out, "out", cache, cache.dtype, (Tq, heads, cache.d)), le.data_ptr() if lse else 0,
+                              op, le.data_ptr() if lse else 0,
                               _array(ws, "ws", cache, torch.uint8, ws.shape), ws.numel(), _raw_stream(cache)))
     return (out, le) if lse else out
