@@ -658,36 +658,48 @@ void kv_attend_kernel(AttendArgs A) {
 
 // Joins the splits of one subtile of one row block.  All their maxima and sums are read at once, 16 columns by 4 splits a wave, and become
 // the splits' factors in LDS; then each of the waves adds its share of the splits' products, and the first wave what they have.  Few
-// splits (many sequences) take one wave, many eight.
+// splits (many sequences) take one wave, many eight.  What the workspace holds is read before it is known which splits have written
+// anything; the others are left out afterwards, whatever their places hold.
 template <bool BF, int ND, int NT, int WAVES, int MOST>
-__global__ __launch_bounds__(64 * WAVES) void kv_join_kernel(AttendArgs A) {
-    constexpr int R = 16 * NT, LANES = 4 * WAVES;
+__global__ __launch_bounds__(64 * WAVES, 4) void kv_join_kernel(AttendArgs A) {
+    constexpr int R = 16 * NT, LANES = 4 * WAVES, EACH = MOST / LANES, EARLY = 4;
     __shared__ floatx4 swap[WAVES][64];
     __shared__ float factor[MOST][16], most[WAVES][16], all[WAVES][16];
     const KVAttend& a = A.a;
     const int b = blockIdx.z, h = blockIdx.y, tile = blockIdx.x % (2 * ND * NT), rb = blockIdx.x / (2 * ND * NT);
     const int s = tile / NT, c = tile % NT;
-    const int wave = threadIdx.x / 64, lane = threadIdx.x & 63, n = lane & 15, q = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63, n = lane & 15, q = lane >> 4;
+    const int64_t stride = R * (32 * ND + 2);
+    const float* part = a.part + (((int64_t)b * A.c.heads + h) * A.row_blocks + rb) * A.splits * stride;
+    const float* products = part + 2 * R + ((s * NT + c) * 64 + lane) * 4;
+    const int col = c * 16 + n;
+
+    float tops[EACH], sums[EACH];
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) {
+        const int i = k * LANES + wave * 4 + q;
+        tops[k] = i < A.splits ? part[i * stride + col] : kNone;
+        sums[k] = i < A.splits ? part[i * stride + R + col] : 0.f;
+    }
+    floatx4 early[EARLY];
+#pragma unroll
+    for (int k = 0; k < EARLY; ++k) early[k] = *(const floatx4*)(products + min(k * WAVES + wave, A.splits - 1) * stride);
+
     const Place place(a, A.c, A.group.by, b);
     const int rows = place.rows, len = place.len, q0 = place.q0, nq = place.nq, row0 = rb * R;
     if (row0 + c * 16 >= rows) return;
-    const int i0 = A.group.quotient(row0), i1 = A.group.quotient(max(min(row0 + R, rows) - 1, 0));
+    const int i0 = A.group.quotient(row0), i1 = A.group.quotient(min(row0 + R, rows) - 1);
     const int hi = a.causal ? max(min(len, len - nq + i1 + 1), 0) : len;
     const int lo = (a.window ? max(0, len - nq + i0 - a.window + 1) : 0) & ~(kStep - 1);
     if (hi - lo <= A.chunk) return;                               // one split has written the result itself
     const int parts = min(A.splits, (hi - lo + A.chunk - 1) / A.chunk);
-    const int64_t stride = R * (32 * ND + 2);
-    const float* part = a.part + (((int64_t)b * A.c.heads + h) * A.row_blocks + rb) * A.splits * stride;
-    const int col = c * 16 + n;
-    const bool live = row0 + col < rows;
 
-    constexpr int EACH = MOST / LANES;
-    float tops[EACH], sums[EACH], t = kNone, l = 0.f;
+    float t = kNone, l = 0.f;
 #pragma unroll
     for (int k = 0; k < EACH; ++k) {
-        const int i = k * LANES + wave * 4 + q;
-        tops[k] = i < parts && live ? part[i * stride + col] : kNone;
-        sums[k] = i < parts && live ? part[i * stride + R + col] : 0.f;
+        const bool has = k * LANES + wave * 4 + q < parts;
+        tops[k] = has ? tops[k] : kNone;
+        sums[k] = has ? sums[k] : 0.f;
         t = fmaxf(t, tops[k]);
     }
     t = fmaxf(t, __shfl_xor(t, 16));
@@ -708,19 +720,23 @@ __global__ __launch_bounds__(64 * WAVES) void kv_join_kernel(AttendArgs A) {
     __syncthreads();
 
     floatx4 o = {0, 0, 0, 0};
-    const floatx4* from = (const floatx4*)(part + 2 * R) + (s * NT + c) * 64 + lane;
-    if (live)
-#pragma unroll 8
-        for (int i = wave; i < parts; i += WAVES) o += factor[i][n] * *(const floatx4*)((const float*)from + i * stride);
+#pragma unroll
+    for (int k = 0; k < EARLY; ++k) {
+        const int i = k * WAVES + wave;
+        if (i < parts) o += factor[i][n] * early[k];
+    }
+#pragma unroll 2
+    for (int i = EARLY * WAVES + wave; i < parts; i += WAVES) o += factor[i][n] * *(const floatx4*)(products + i * stride);
     swap[wave][lane] = o;
     __syncthreads();
-    if (wave || !live) return;
+    const int row = row0 + col;
+    if (wave || row >= rows) return;
     l = 0.f;
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) l += all[w][n];
 #pragma unroll
     for (int w = 1; w < WAVES; ++w) o += swap[w][lane];
-    const int row = row0 + col, i = A.group.quotient(row), g = row - i * A.group.by;
+    const int i = A.group.quotient(row), g = row - i * A.group.by;
     const int64_t at = (int64_t)(q0 + i) * a.q_heads + h * A.group.by + g;
     const float inv = inverse(l);
 #pragma unroll
