@@ -24,8 +24,8 @@
 //
 // What bounds it.  Single tokens (at most 16 query rows to a cache head): bytes, 2 (d/2 + 2) a token and head.  64 sequences of up to 8192
 // tokens, 8 heads of 128: 353 MB in 81 us, 4.3 TB/s (5.0 where they are equally long; a large copy reaches 5.2); one of 131072: 138 MB in 31 us
-// and the join 5.  Few tokens: a workgroup's fixed cost, about 6 us with its launch, of which the chain of first loads (page, codes; not the length, see
-// below), the table (64 KiB of LDS) and the exchange between the waves are a third each, then 1.1 us a step of 8 x 32 tokens.
+// and the join 4.5.  Few tokens: a workgroup's fixed cost, about 6 us with its launch, of which the chain of first loads (page, codes; the length
+// is not waited for), the table (64 KiB of LDS) and the exchange between the waves are a third each, then 1.1 us a step of 8 x 32 tokens.
 // Many rows: vector instructions.  A step of 48 rows and 32 tokens at d = 128 takes 48 MFMA (768 cycles), 64 lookups and about 240 vector
 // instructions with 24 exponentials (1340 cycles); two waves a SIMD overlap a third of the two.  Two sequences of 4096 queries over up to
 // 9000 tokens, 32 query heads: 852 GFLOP in 1042 us, 0.82 PFLOP/s; a large product of the library reaches 1.2 on this card.
@@ -38,7 +38,7 @@ namespace fk {
 
 constexpr float kSlack = 8.f;            // in powers of two
 constexpr float kScaleSlack = 64.f;
-constexpr float kNone = -3.402823466e38f;  // maximum of a row that has seen nothing
+constexpr float kNone = -3.402823466e38f;   // below every score: the maximum of a row that has seen nothing
 constexpr int kJoinWaves = 8;            // waves of a workgroup that share the rows
 constexpr int kOwnWaves = 4;             // waves of a workgroup with rows of their own
 constexpr int kStep = 32;                // tokens a wave takes at a time
@@ -131,25 +131,12 @@ __device__ __forceinline__ int channel_of(int s, int m) {
     return 2 * (16 * P::before(p) + m * P::width(p) + (byte - P::before(p))) + (s & 1);
 }
 
-// The largest of 16 lanes (not NaN), in all of them; lane exchanges of the vector ALU, a few cycles each where LDS takes a hundred
-template <int CTRL>
-__device__ __forceinline__ float max_with(float v) {
-    return fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false)));
-}
-__device__ __forceinline__ float row_max(float v) {
-    v = max_with<0xB1>(v);                                        // lane ^ 1
-    v = max_with<0x4E>(v);                                        // lane ^ 2
-    v = max_with<0x141>(v);                                       // mirrored in 8
-    return max_with<0x140>(v);                                    // mirrored in 16
-}
-__device__ __forceinline__ float lane_of(float v, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane)); }
-
-// An address that is the same in all lanes, as scalar registers: loads then take a 32-bit offset of the lane and need no 64-bit vector
-// addition each.
+// An address that is the same in all lanes, summed in scalar registers.  (Left to itself the compiler adds the lane's offset to the array's
+// address outside the loop, and keeps a pair of vector registers for every array.)
 typedef __attribute__((address_space(1))) const uint8_t* Base;
 __device__ __forceinline__ Base base_of(const void* p, int64_t bytes) {
     uint64_t v = (uint64_t)p + bytes;
-    __asm__("" : "+s"(v));                                        // (or the compiler adds the lane's offset to p outside the loop)
+    __asm__("" : "+s"(v));
     return (Base)v;
 }
 template <class T>
@@ -237,34 +224,28 @@ struct Reader {
 template <bool BF>
 __device__ __forceinline__ float scale_at(uintx2 s, int r) { return lp_to_float((uint16_t)(s[r / 2] >> 16 * (r & 1)), BF); }
 
-// A table of pairs of levels in LDS: 256 rows of COPIES pairs of the keys' levels and as many of the values'.
-template <int COPIES>
+// The table of pairs of levels in LDS: 256 rows of 32 pairs of the keys' levels and 32 of the values'.
 struct Table {
-    static constexpr int bytes = 256 * COPIES * 8;
-    static_assert(COPIES == 32 || COPIES == 16, "rows of 256 bytes, or two to that");
+    static constexpr int bytes = 65536;
 
-    // what `pair` takes as `copy`: the lane's copy in a row of 256 bytes
-    static __device__ __forceinline__ uint32_t copy_of(int lane) { return (lane % COPIES) * 4 * (32 / COPIES); }
-
-    // the pair of byte b of the word
+    // the pair of byte b of the word; copy = 4 (lane % 32)
     template <bool VALUES>
     static __device__ __forceinline__ uint32_t pair(const uint8_t* lds, uint32_t word, int b, uint32_t copy) {
-        const uint32_t at = __builtin_amdgcn_perm(word, copy, 0x0c0c0400u | (uint32_t)b << 8) / (32 / COPIES);
-        return *(const uint32_t*)(lds + at + (VALUES ? COPIES * 4 : 0));
+        return *(const uint32_t*)(lds + __builtin_amdgcn_perm(word, copy, 0x0c0c0400u | (uint32_t)b << 8) + (VALUES ? 128 : 0));
     }
 
     // The level that a lane brings to `fill`: lanes 0..15 the keys', lanes 16..31 the values'.
     static __device__ __forceinline__ uint16_t level(const KVView& c, int h, int lane) {
         return ((lane & 16) ? c.v_levels : c.k_levels)[h * 16 + (lane & 15)];
     }
+    // A row is sixteen pieces of 16 bytes, eight of the keys and eight of the values.
     template <bool BF, int THREADS>
     static __device__ __forceinline__ void fill(uint8_t* lds, uint16_t level, int lane) {
-        constexpr int pieces = COPIES / 2, keys = pieces / 2;     // of 16 bytes: of a row, and of its keys' part
         const uint32_t mine = (lane & 16) ? float_to_half(lp_to_float(level, BF)) : level;
-        const int side = lane & keys ? 16 : 0;
+        const int side = lane & 8 ? 16 : 0;
 #pragma unroll 2
         for (int i = 0; i < bytes / 16 / THREADS; ++i) {
-            const int at = i * THREADS + threadIdx.x, code = at / pieces;
+            const int at = i * THREADS + threadIdx.x, code = at / 16;
             const uint32_t pair = (uint32_t)__shfl((int)mine, side + (code & 15)) | ((uint32_t)__shfl((int)mine, side + (code >> 4)) << 16);
             ((uintx4*)lds)[at] = uintx4{pair, pair, pair, pair};
         }
@@ -430,7 +411,7 @@ template <bool BF, int ND, int NT, bool JOIN>
 __global__ __launch_bounds__(64 * (JOIN ? kJoinWaves : kOwnWaves), JOIN ? (NT == 1 && ND <= 4 ? 4 : 1) : 2)
 void kv_attend_kernel(AttendArgs A) {
     // (a fixed size, so that the compiler knows the table's address and leaves it to the instruction's offset)
-    using T = Table<32>;
+    using T = Table;
     __shared__ __align__(16) uint8_t lds[T::bytes + (JOIN ? 2 * kJoinWaves * 16 * NT * 4 : 0)];
     using P = Pieces<ND>;
     constexpr int R = 16 * NT, S = 2 * ND, W = JOIN ? kJoinWaves : 1, THREADS = 64 * (JOIN ? kJoinWaves : kOwnWaves);
@@ -480,7 +461,7 @@ void kv_attend_kernel(AttendArgs A) {
     seen.lo = lo;
     seen.hi = hi;
     load_queries<ND, NT>(A, at, h, row0, n, q, Q, seen);
-    T::template fill<BF, THREADS>(lds, level, lane);
+    T::fill<BF, THREADS>(lds, level, lane);
 
     floatx4 O[S][NT];
     Softmax<NT, S> soft;
@@ -488,7 +469,7 @@ void kv_attend_kernel(AttendArgs A) {
     for (int c = 0; c < NT; ++c)
 #pragma unroll
         for (int s = 0; s < S; ++s) O[s][c] = floatx4{0, 0, 0, 0};
-    const uint32_t copy = T::copy_of(lane);
+    const uint32_t copy = (lane & 31) * 4;
     __syncthreads();
 
     for (int it = 0; it < steps; ++it) {
@@ -559,31 +540,31 @@ void kv_attend_kernel(AttendArgs A) {
     __asm__("" : "+s"(last0));                                    // (places of the result are found now, not kept in registers all along)
     if constexpr (!JOIN) {
 #pragma unroll
-    for (int c = 0; c < NT; ++c) {
-        const int row = last0 + c * 16 + n, i = A.group.quotient(row), g = row - i * A.group.by;
-        if (row >= rows) continue;
-        const int64_t to = (int64_t)(q0 + i) * a.q_heads + h * A.group.by + g;
-        const float inv = inverse(soft.sum[c]);
-        // a piece's channels of one of O^T's rows lie side by side
+        for (int c = 0; c < NT; ++c) {
+            const int row = last0 + c * 16 + n, i = A.group.quotient(row), g = row - i * A.group.by;
+            if (row >= rows) continue;
+            const int64_t to = (int64_t)(q0 + i) * a.q_heads + h * A.group.by + g;
+            const float inv = inverse(soft.sum[c]);
+            // a piece's channels of one of O^T's rows lie side by side
 #pragma unroll
-        for (int p = 0; p < P::count; ++p)
+            for (int p = 0; p < P::count; ++p)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                uint32_t o[P::width(0)];
+                for (int r = 0; r < 4; ++r) {
+                    uint32_t o[P::width(0)];
 #pragma unroll
-                for (int j = 0; j < P::width(p); ++j) {
-                    const int s = 2 * (P::before(p) + j);
-                    o[j] = float_to_lp_any(O[s][c][r] * inv, BF) | (uint32_t)float_to_lp_any(O[s + 1][c][r] * inv, BF) << 16;
+                    for (int j = 0; j < P::width(p); ++j) {
+                        const int s = 2 * (P::before(p) + j);
+                        o[j] = float_to_lp_any(O[s][c][r] * inv, BF) | (uint32_t)float_to_lp_any(O[s + 1][c][r] * inv, BF) << 16;
+                    }
+                    uint16_t* out = a.out + to * (32 * ND) + 2 * (16 * P::before(p) + (4 * q + r) * P::width(p));
+                    if constexpr (P::width(0) == 4)
+                        if (P::width(p) == 4) *(uintx4*)out = uintx4{o[0], o[1], o[2], o[3]};
+                    if constexpr (P::width(0) >= 2)
+                        if (P::width(p) == 2) *(uintx2*)out = uintx2{o[0], o[1]};
+                    if (P::width(p) == 1) *(uint32_t*)out = o[0];
                 }
-                uint16_t* out = a.out + to * (32 * ND) + 2 * (16 * P::before(p) + (4 * q + r) * P::width(p));
-                if constexpr (P::width(0) == 4)
-                    if (P::width(p) == 4) *(uintx4*)out = uintx4{o[0], o[1], o[2], o[3]};
-                if constexpr (P::width(0) >= 2)
-                    if (P::width(p) == 2) *(uintx2*)out = uintx2{o[0], o[1]};
-                if (P::width(p) == 1) *(uint32_t*)out = o[0];
-            }
-        if (a.lse && q == 0) a.lse[to] = lse_of(soft.top[c], soft.sum[c]);
-    }
+            if (a.lse && q == 0) a.lse[to] = lse_of(soft.top[c], soft.sum[c]);
+        }
         return;
     }
 
