@@ -64,7 +64,7 @@ struct KVAttend {
 struct KVPlan {
     int tiles;            // tiles of 16 query rows (query token, head of the group) in a wave
     bool join;            // the waves of a workgroup share the rows and divide the tokens; otherwise each has rows of its own
-    int row_blocks;       // workgroups along the rows of a sequence and cache head
+    int row_blocks;       // along the rows of a sequence and cache head: workgroups, or tiles of waves with rows of their own
     int splits;           // workgroups along the tokens
     int64_t chunk;        // tokens of a split, a multiple of what the waves of a workgroup take at a time
 };

@@ -40,7 +40,8 @@ constexpr float kSlack = 8.f;            // in powers of two
 constexpr float kScaleSlack = 64.f;
 constexpr float kNone = -3.402823466e38f;   // below every score: the maximum of a row that has seen nothing
 constexpr int kJoinWaves = 8;            // waves of a workgroup that share the rows
-constexpr int kOwnWaves = 4;             // waves of a workgroup with rows of their own
+// Waves of a workgroup with rows of their own: four, two workgroups to a compute unit; with one tile each eight, that share one table.
+constexpr int own_waves(int tiles) { return tiles == 1 ? 8 : 4; }
 constexpr int kStep = 32;                // tokens a wave takes at a time
 constexpr int kMostSplits = 256;          // of one row block's tokens
 constexpr int kPagesAhead = 32;          // steps whose pages a wave holds in one register (two halves each)
@@ -406,20 +407,34 @@ struct Softmax {
 };
 
 // JOIN: the waves of a workgroup share the rows and divide the tokens, each takes every kJoinWaves-th step (and workgroups may divide them
-// further); otherwise each wave has rows of its own and takes all steps that they see.  Codes go straight from the cache into operands.
+// further); otherwise each wave has rows of its own, of one sequence or, where that has fewer tiles than a workgroup has waves, of
+// several, and takes all steps that they see.  Codes go straight from the cache into operands.
 template <bool BF, int ND, int NT, bool JOIN>
-__global__ __launch_bounds__(64 * (JOIN ? kJoinWaves : kOwnWaves), JOIN ? (NT == 1 && ND <= 4 ? 4 : 1) : 2)
+__global__ __launch_bounds__(64 * (JOIN ? kJoinWaves : own_waves(NT)), NT == 1 && ND <= 4 ? 4 : JOIN ? 1 : 2)
 void kv_attend_kernel(AttendArgs A) {
     // (a fixed size, so that the compiler knows the table's address and leaves it to the instruction's offset)
     using T = Table;
     __shared__ __align__(16) uint8_t lds[T::bytes + (JOIN ? 2 * kJoinWaves * 16 * NT * 4 : 0)];
     using P = Pieces<ND>;
-    constexpr int R = 16 * NT, S = 2 * ND, W = JOIN ? kJoinWaves : 1, THREADS = 64 * (JOIN ? kJoinWaves : kOwnWaves);
-    // (rows of their own: the blocks with the most tokens first)
-    const int blocks = A.c.heads * A.a.B;
-    const int h = JOIN ? blockIdx.y : blockIdx.x % A.c.heads, b = JOIN ? blockIdx.z : blockIdx.x / A.c.heads % A.a.B;
-    const int split = JOIN ? blockIdx.x % A.splits : 0, rb = JOIN ? blockIdx.x / A.splits : A.row_blocks - 1 - blockIdx.x / blocks;
+    constexpr int R = 16 * NT, S = 2 * ND, W = JOIN ? kJoinWaves : 1, WAVES = JOIN ? kJoinWaves : own_waves(NT), THREADS = 64 * WAVES;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63, n = lane & 15, q = lane >> 4;
+    // row_blocks: of a sequence, workgroups where its waves share the rows, tiles otherwise
+    int h, b, split = 0, rb;
+    bool some = true;                                             // whether there is such a sequence
+    const bool packed = !JOIN && A.row_blocks < WAVES;
+    if constexpr (JOIN) {
+        h = blockIdx.y, b = blockIdx.z, split = blockIdx.x % A.splits, rb = blockIdx.x / A.splits;
+    } else {
+        h = blockIdx.x % A.c.heads;
+        const int block = blockIdx.x / A.c.heads;
+        if (packed) {
+            const int unit = block * WAVES + wave, sequence = unit / A.row_blocks;
+            some = sequence < A.a.B;
+            b = min(sequence, A.a.B - 1), rb = unit - sequence * A.row_blocks;
+        } else {                                                  // the tiles with the most tokens first
+            b = block % A.a.B, rb = ((A.row_blocks - 1) / WAVES - block / A.a.B) * WAVES + wave;
+        }
+    }
     const KVAttend& a = A.a;
     const uint16_t level = T::level(A.c, h, lane);                // (the first load: the table waits for it alone)
 
@@ -439,8 +454,8 @@ void kv_attend_kernel(AttendArgs A) {
     if (!a.window) begin();
 
     const Place at(a, A.c, A.group.by, b);
-    const int rows = at.rows, len = at.len, q0 = at.q0, nq = at.nq, row0 = (JOIN ? rb : rb * kOwnWaves + wave) * R;
-    if ((JOIN ? row0 : rb * kOwnWaves * R) >= rows) return;       // the whole workgroup
+    const int rows = some ? at.rows : 0, len = at.len, q0 = at.q0, nq = at.nq, row0 = rb * R;
+    if (JOIN ? row0 >= rows : !packed && (rb - wave) * R >= rows) return;   // the whole workgroup
 
     // tokens that the wave's rows see
     const int i0 = A.group.quotient(row0), i1 = A.group.quotient(max(min(row0 + R, rows) - 1, 0));
@@ -733,24 +748,43 @@ static constexpr int join_tiles(int ND) { return ND <= 2 ? 4 : ND <= 4 ? 3 : ND 
 
 KVPlan choose_kv_plan(const KVView& c, int q_heads, int B, int max_q, int64_t reach) {
     const int group = q_heads / c.heads, ND = c.d / 32;
-    const int64_t rows = (int64_t)max_q * group;
+    const int64_t rows = (int64_t)max_q * group, units = device_cu_count();
     KVPlan p;
-    // Waves with rows of their own need no exchange at the end, but the rows' workgroups alone have to fill the chip (8 x 5 queries of 16
-    // heads of 256 over 4000 tokens: 16 workgroups 360 us, divided by tokens too 22); otherwise the tokens are divided.
-    p.join = rows <= 16 * join_tiles(ND) || (int64_t)B * c.heads * cdiv(rows, 16 * own_tiles(ND) * kOwnWaves) < device_cu_count();
-    p.tiles = !p.join ? own_tiles(ND) : (int)std::min(cdiv(rows, 16), (int64_t)join_tiles(ND));
-    p.row_blocks = (int)cdiv(rows, 16 * p.tiles * (p.join ? 1 : kOwnWaves));
     p.splits = 1;
     p.chunk = INT32_MAX / 2;
-    if (p.join) {
-        // One workgroup to a compute unit: 8 heads, one sequence of 131072 tokens 64 splits 40.6 us, 32 37.8, 24 43.7.
-        const int64_t wg = kJoinWaves * kStep, slots = (int64_t)device_cu_count(), blocks = (int64_t)B * c.heads * p.row_blocks;
-        const int64_t want = blocks >= slots ? 1 : slots / blocks, steps = cdiv(reach, wg);
-        // Splitting costs the second launch, about four steps of a workgroup: 8 heads of 128, one sequence of 700 tokens (3 steps) 10.6 us
-        // in one piece and 11.1 in three, of 1500 (6) 14.7 and 11.9 in six; 24 sequences of 2048 (8), 4 heads of 64, 13.5 and 13.9 in two.
-        p.splits = (int)std::min({want, steps, (int64_t)kMostSplits});
-        if (steps - cdiv(steps, p.splits) <= 4) p.splits = 1;
-        if (p.splits > 1) p.chunk = cdiv(steps, p.splits) * wg;
+    // Waves with rows of their own need no exchange at the end, but the rows' workgroups alone have to fill the chip (8 x 5 queries of 16
+    // heads of 256 over 4000 tokens: 16 workgroups 360 us, divided by tokens too 22); otherwise the tokens are divided.
+    const int64_t own_blocks = (int64_t)B * c.heads * cdiv(rows, 16 * own_tiles(ND) * own_waves(own_tiles(ND)));
+    if (rows > 16 * join_tiles(ND) && own_blocks >= units) {
+        p.join = false;
+        p.tiles = own_tiles(ND);
+        p.row_blocks = (int)cdiv(rows, 16 * p.tiles);
+        return p;
+    }
+    p.join = true;
+    p.tiles = (int)std::min(cdiv(rows, 16), (int64_t)join_tiles(ND));
+    p.row_blocks = (int)cdiv(rows, 16 * p.tiles);
+    // One workgroup to a compute unit: 8 heads, one sequence of 131072 tokens 64 splits 40.6 us, 32 37.8, 24 43.7.
+    const int64_t wg = kJoinWaves * kStep, blocks = (int64_t)B * c.heads * p.row_blocks;
+    const int64_t want = blocks >= units ? 1 : units / blocks, steps = cdiv(reach, wg);
+    // Splitting costs the second launch, about four steps of a workgroup: 8 heads of 128, one sequence of 700 tokens (3 steps) 10.6 us
+    // in one piece and 11.1 in three, of 1500 (6) 14.7 and 11.9 in six; 24 sequences of 2048 (8), 4 heads of 64, 13.5 and 13.9 in two.
+    p.splits = (int)std::min({want, steps, (int64_t)kMostSplits});
+    if (steps - cdiv(steps, p.splits) <= 4) p.splits = 1;
+    if (p.splits > 1) {
+        p.chunk = cdiv(steps, p.splits) * wg;
+        return p;
+    }
+    // Many short sequences: a tile to a wave, eight to a workgroup, saves the workgroups' fixed cost and gives up dividing the tokens.  In tenths
+    // of a microsecond, fitted: a round of workgroups that share their rows takes 50 and 8 a step of 256 tokens, one of tiles 42 and 14 a step of
+    // 32.  Measured, one query of 4 heads to each of 8 heads of 128: 64 sequences of 100 tokens 10.2 us shared and 10.5 in tiles, of 200 12.7
+    // and 14.7, 128 of 300 22.8 and 18.3, 110 (9 heads) of up to 9 17.6 and 7.8.
+    const int64_t tiles = cdiv(rows, 16), own = cdiv(B * tiles, 8) * c.heads;
+    const int64_t shared_cost = (50 + 8 * steps) * std::max(blocks, units), own_cost = (42 + 14 * cdiv(reach, kStep)) * std::max(own, units);
+    if (own_cost < shared_cost) {
+        p.join = false;
+        p.tiles = 1;
+        p.row_blocks = (int)tiles;
     }
     return p;
 }
@@ -771,12 +805,15 @@ static fk_status launch_form(const AttendArgs& A, hipStream_t s) {
 template <bool BF, int ND>
 static fk_status launch_width(const AttendArgs& A, const KVPlan& p, hipStream_t s) {
     if (!p.join) {
-        const int64_t blocks = (int64_t)A.row_blocks * A.c.heads * A.a.B;
+        const int waves = own_waves(p.tiles);
+        const int64_t blocks = (A.row_blocks < waves ? cdiv((int64_t)A.a.B * A.row_blocks, waves) : cdiv(A.row_blocks, waves) * A.a.B) * A.c.heads;
         if (blocks > INT32_MAX / 512) {
             set_error("fk_kv_attend: unsupported size: %lld workgroups", (long long)blocks);
             return FK_EUNSUPPORTED;
         }
-        kv_attend_kernel<BF, ND, own_tiles(ND), false><<<(unsigned)blocks, 64 * kOwnWaves, 0, s>>>(A);
+        if (p.tiles == 1) kv_attend_kernel<BF, ND, 1, false><<<(unsigned)blocks, 64 * own_waves(1), 0, s>>>(A);
+        else if constexpr (own_tiles(ND) > 1)
+            kv_attend_kernel<BF, ND, own_tiles(ND), false><<<(unsigned)blocks, 64 * own_waves(own_tiles(ND)), 0, s>>>(A);
         FK_HIP(hipGetLastError());
         return FK_OK;
     }
