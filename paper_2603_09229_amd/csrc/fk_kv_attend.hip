@@ -23,12 +23,13 @@
 // 11 bits, as many as the values have in an uncoded cache of fp16, and sums and statistics are fp32.
 //
 // What bounds it.  Single tokens (at most 16 query rows to a cache head): bytes, 2 (d/2 + 2) a token and head.  64 sequences of up to 8192
-// tokens, 8 heads of 128: 353 MB in 81 us, 4.3 TB/s (5.0 where they are equally long; a large copy reaches 5.2); one of 131072: 138 MB in 31 us
-// and the join 4.5.  Few tokens: a workgroup's fixed cost, about 6 us with its launch, of which the chain of first loads (page, codes; the length
+// tokens, 8 heads of 128: 353 MB in 83 us, 4.2 TB/s (5.0 where they are equally long; a large copy reaches 5.2); one of 131072: 138 MB in 31 us
+// and the join 4.7.  Few tokens: a workgroup's fixed cost, about 6 us with its launch, of which the chain of first loads (page, codes; the length
 // is not waited for), the table (64 KiB of LDS) and the exchange between the waves are a third each, then 1.1 us a step of 8 x 32 tokens.
+// Many sequences of few tokens share workgroups, a wave each: 110 of up to 9, 9 heads, 7.8 us.
 // Many rows: vector instructions.  A step of 48 rows and 32 tokens at d = 128 takes 48 MFMA (768 cycles), 64 lookups and about 240 vector
 // instructions with 24 exponentials (1340 cycles); two waves a SIMD overlap a third of the two.  Two sequences of 4096 queries over up to
-// 9000 tokens, 32 query heads: 852 GFLOP in 1042 us, 0.82 PFLOP/s; a large product of the library reaches 1.2 on this card.
+// 9000 tokens, 32 query heads: 852 GFLOP in 1042 to 1066 us, 0.8 PFLOP/s; a large product of the library reaches 1.2 on this card.
 #include <algorithm>
 
 #include "fk_device.h"
