@@ -1,6 +1,8 @@
 // C-ABI entry points of the 4-bit key/value cache: argument checks and launches.
 #include <string.h>
 
+#include <algorithm>
+
 #include "fk_kv.h"
 
 namespace fk {
@@ -168,6 +170,8 @@ fk_status fk_kv_attend(const fk_kv_cache* cache, const void* q, int64_t q_token_
         return FK_EUNSUPPORTED;
     }
     if (max_len == 0) max_len = (int64_t)max_pages << c.page_shift;
+    // No two positions are further apart: positions are from -2^30 (max_q) to 2^30, and 32 bits hold one of them less the window.
+    window = std::min(window, 1 << 30);
     if (Tq == 0) return FK_OK;
     FK_TRY(need(fn, "q", q, 2));
     FK_TRY(need(fn, "pages", pages, 4));
