@@ -363,6 +363,12 @@ fk_status fk_kv_attend(const fk_kv_cache* cache, const void* q, int64_t q_token_
 /* Device bytes that fk_kv_attend needs in ws (256-byte aligned, contents undefined before and after); 0 if unsupported.  Of the cache
  * only the sizes and t are read; max_len >= 1. */
 size_t fk_kv_workspace_bytes(const fk_kv_cache* cache, int q_heads, int64_t Tq, int B, int max_q, int64_t max_len);
+/* What fk_kv_attend would launch for these sizes, as fk_plan has it for the other entry points: one line in buf (host memory,
+ * NUL-terminated, truncated to buf_bytes).  "rows_shared": the waves of a workgroup share its rows and divide the tokens, `splits`
+ * workgroups of `chunk` tokens divide them further; "rows_own": each of its waves has rows of its own, of one sequence or, "packed", of
+ * several.  tiles: of 16 query rows in a wave; row_blocks: workgroups, or waves, that a sequence and cache head take along its rows.
+ * Host-only; of the cache only the sizes and t are read; max_len >= 1. */
+int fk_kv_plan(const fk_kv_cache* cache, int q_heads, int B, int max_q, int64_t max_len, int window, char* buf, size_t buf_bytes);
 
 #ifdef __cplusplus
 }

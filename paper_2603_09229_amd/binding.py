@@ -23,7 +23,7 @@ EXPORTS = ("fk_last_error", "fk_workspace_bytes", "fk_assign", "fk_sort_inverse"
            "fk_lloyd_iter", "fk_lloyd_ooc", "fk_ooc_workspace_bytes", "fk_stage_timer_start",
            "fk_stage_timer_stop", "fk_plan", "fk_set_option", "fk_standard_assign",
            "fk_standard_update", "fk_assign_static", "fk_assign_static_limit", "fk_kv_append", "fk_kv_read",
-           "fk_kv_attend", "fk_kv_workspace_bytes")
+           "fk_kv_attend", "fk_kv_workspace_bytes", "fk_kv_plan")
 STAGES = ("assign", "sort", "reduce", "finalize")
 
 
@@ -85,6 +85,8 @@ def lib() -> ctypes.CDLL:
                                    vp, sz, vp]
         L.fk_kv_workspace_bytes.restype = sz
         L.fk_kv_workspace_bytes.argtypes = [cache, i32, i64, i32, i32, i64]
+        L.fk_kv_plan.restype = i32
+        L.fk_kv_plan.argtypes = [cache, i32, i32, i32, i64, i32, ctypes.c_char_p, sz]
         L.fk_plan.restype = i32
         L.fk_plan.argtypes = [i32, i64, i32, i32, i32, ctypes.c_char_p, sz]
         L.fk_set_option.restype = i32
@@ -418,6 +420,13 @@ def make_kv_workspace(cache: KVCache, B: int, q_heads: int, Tq: int, max_q: int,
     if n == 0:
         raise FlashKMError(2, f"unsupported attention: {lib().fk_last_error().decode()}")
     return torch.empty(n, dtype=torch.uint8, device=cache.device)
+
+
+def fk_kv_plan(cache: KVCache, B: int, q_heads: int, max_q: int, max_len: int, window: int = 0) -> str:
+    """One-line description of what fk_kv_attend would launch for these sizes."""
+    buf = ctypes.create_string_buffer(256)
+    _check(lib().fk_kv_plan(cache._ref, q_heads, B, max_q, max_len, window, buf, len(buf)))
+    return buf.value.decode()
 
 
 def fk_kv_attend(cache: KVCache, q, pages, lens, *, q_start=None, max_q=None, max_len: int = 0, scale=None, causal: bool = True,

@@ -60,6 +60,9 @@ struct KVAttend {
     float* part;          // workspace: see kv_partial_floats
 };
 
+// Waves of a workgroup with rows of their own: four, two workgroups to a compute unit; with one tile each eight, that share one table.
+constexpr int own_waves(int tiles) { return tiles == 1 ? 8 : 4; }
+
 // How an attention call is divided.
 struct KVPlan {
     int tiles;            // tiles of 16 query rows (query token, head of the group) in a wave

@@ -1,5 +1,5 @@
 // C-ABI entry points of the 4-bit key/value cache: argument checks and launches.
-#include <string.h>
+#include <stdio.h>
 
 #include <algorithm>
 
@@ -67,6 +67,11 @@ static fk_status check_queries(const char* fn, const KVView& c, int q_heads, int
         return FK_EUNSUPPORTED;
     }
     return FK_OK;
+}
+
+// The most tokens that the queries of a sequence see together.
+static int64_t reach_of(int window, int max_q, int64_t max_len) {
+    return window ? std::min((int64_t)window + max_q - 1, max_len) : max_len;
 }
 
 }  // namespace fk
@@ -152,6 +157,32 @@ size_t fk_kv_workspace_bytes(const fk_kv_cache* cache, int q_heads, int64_t Tq, 
     return align_up(n, 256) + 256;
 }
 
+int fk_kv_plan(const fk_kv_cache* cache, int q_heads, int B, int max_q, int64_t max_len, int window, char* buf, size_t buf_bytes) {
+    const char* fn = "fk_kv_plan";
+    if (!buf || buf_bytes == 0) {
+        set_error("%s: no buffer", fn);
+        return FK_EINVAL;
+    }
+    snprintf(buf, buf_bytes, "unsupported");
+    KVView c;
+    fk_status why;
+    if (!view_of(fn, cache, false, &c, &why)) return why;
+    FK_TRY(check_queries(fn, c, q_heads, 0, B, max_q, max_len));
+    if (max_len < 1 || window < 0) {
+        set_error("%s: max_len=%lld is not positive or window=%d is negative", fn, (long long)max_len, window);
+        return FK_EINVAL;
+    }
+    const KVPlan p = choose_kv_plan(c, q_heads, B, max_q, reach_of(window, max_q, max_len));
+    const size_t bytes = align_up(kv_partial_bytes(p, c.d, c.heads, B), 256) + 256;
+    if (p.join)
+        snprintf(buf, buf_bytes, "rows_shared(tiles=%d,row_blocks=%d,splits=%d,chunk=%lld) workspace=%zu", p.tiles, p.row_blocks, p.splits,
+                 (long long)(p.splits > 1 ? p.chunk : 0), bytes);
+    else
+        snprintf(buf, buf_bytes, "rows_own(tiles=%d,row_blocks=%d,waves=%d%s) workspace=%zu", p.tiles, p.row_blocks, own_waves(p.tiles),
+                 p.row_blocks < own_waves(p.tiles) ? ",packed" : "", bytes);
+    return FK_OK;
+}
+
 fk_status fk_kv_attend(const fk_kv_cache* cache, const void* q, int64_t q_token_stride, int64_t q_head_stride,
                        int q_heads, int64_t Tq, const int32_t* pages, int max_pages, const int32_t* lens,
                        const int32_t* q_start, int B, int max_q, int64_t max_len, float scale, int causal, int window,
@@ -180,8 +211,7 @@ fk_status fk_kv_attend(const fk_kv_cache* cache, const void* q, int64_t q_token_
     FK_TRY(need(fn, "out", out, 16));
     if (lse) FK_TRY(need(fn, "lse", lse, 4));
     FK_TRY(need(fn, "ws", ws, 256));
-    const int64_t reach = window ? (int64_t)window + max_q - 1 : max_len;
-    const KVPlan p = choose_kv_plan(c, q_heads, B, max_q, reach < max_len ? reach : max_len);
+    const KVPlan p = choose_kv_plan(c, q_heads, B, max_q, reach_of(window, max_q, max_len));
     const size_t bytes = kv_partial_bytes(p, c.d, c.heads, B);
     if (ws_bytes < bytes) {
         set_error("%s: workspace too small: %zu bytes given, %zu needed", fn, ws_bytes, bytes);

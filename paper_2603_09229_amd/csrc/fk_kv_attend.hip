@@ -41,8 +41,6 @@ constexpr float kSlack = 8.f;            // in powers of two
 constexpr float kScaleSlack = 64.f;
 constexpr float kNone = -3.402823466e38f;   // below every score: the maximum of a row that has seen nothing
 constexpr int kJoinWaves = 8;            // waves of a workgroup that share the rows
-// Waves of a workgroup with rows of their own: four, two workgroups to a compute unit; with one tile each eight, that share one table.
-constexpr int own_waves(int tiles) { return tiles == 1 ? 8 : 4; }
 constexpr int kStep = 32;                // tokens a wave takes at a time
 constexpr int kMostSplits = 256;          // of one row block's tokens
 constexpr int kPagesAhead = 32;          // steps whose pages a wave holds in one register (two halves each)

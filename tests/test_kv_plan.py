@@ -1,0 +1,46 @@
+"""fk_kv_plan: the form, tiles and splits that fk_kv_attend takes, as text, and what it refuses.  No kernel is launched here."""
+import ctypes
+import re
+
+import pytest
+
+from paper_2603_09229_amd import binding as fk
+from tests.test_kv_refusals import EINVAL, EUNSUPPORTED, cache
+
+
+def plan(c=None, heads=32, B=1, max_q=1, max_len=1000, window=0, room=256):
+    buf = ctypes.create_string_buffer(b"?" * room, room)
+    status = fk.lib().fk_kv_plan(ctypes.byref(c or cache(k_codes=None, k_levels=None)), heads, B, max_q, max_len, window, buf, room)
+    return status, buf.value.decode()
+
+
+def test_forms():
+    assert plan()[1].startswith("rows_shared(tiles=1,row_blocks=1,splits=1,chunk=0)")
+    assert re.match(r"rows_shared\(tiles=1,row_blocks=1,splits=(\d\d),chunk=\d+\)", plan(max_len=100000)[1])
+    assert "splits=1," in plan(max_len=100000, window=500)[1]
+    assert plan(B=8, max_q=1024, max_len=4096)[1].startswith("rows_own(tiles=3,row_blocks=86,waves=4)")
+    assert plan(B=32, max_q=25, max_len=4096)[1].startswith("rows_own(tiles=3,row_blocks=3,waves=4,packed)")
+    assert plan(B=500, max_len=20)[1].startswith("rows_own(tiles=1,row_blocks=1,waves=8,packed)")
+    assert plan(c=cache(d=256), B=8, max_q=1024, max_len=4096)[1].startswith("rows_own(tiles=1,row_blocks=256,waves=8)")
+
+
+@pytest.mark.parametrize("B,max_q,max_len", [(1, 1, 1), (1, 1, 1 << 30), (65535, 1, 77), (3, 1 << 27, 1 << 30), (64, 5, 8192), (255, 1, 100000)])
+@pytest.mark.parametrize("d", [32, 96, 128, 256])
+def test_the_workspace_is_the_one_asked_for(B, max_q, max_len, d):
+    c = cache(d=d)
+    status, text = plan(c, 32, B, max_q, max_len)
+    assert status == 0 and int(text.rsplit("=", 1)[1]) == fk.lib().fk_kv_workspace_bytes(ctypes.byref(c), 32, 1, B, max_q, max_len)
+
+
+@pytest.mark.parametrize("other,status", [
+    (dict(heads=12), EINVAL), (dict(B=0), EINVAL), (dict(max_q=0), EINVAL), (dict(max_len=0), EINVAL), (dict(window=-1), EINVAL),
+    (dict(B=70000), EUNSUPPORTED), (dict(max_len=1 << 31), EUNSUPPORTED), (dict(c=cache(d=40)), EUNSUPPORTED),
+])
+def test_what_is_refused(other, status):
+    assert plan(**other) == (status, "unsupported")
+
+
+def test_the_text_is_cut_to_the_buffer():
+    assert plan(room=9) == (0, "rows_sha") and plan(room=1) == (0, "")
+    assert fk.lib().fk_kv_plan(ctypes.byref(cache()), 32, 1, 1, 100, 0, None, 5) == EINVAL
+    assert fk.lib().fk_kv_plan(None, 32, 1, 1, 100, 0, ctypes.create_string_buffer(8), 8) == EINVAL
