@@ -352,9 +352,10 @@ fk_status fk_kv_read(const fk_kv_cache* cache, const int64_t* slots, int64_t T, 
  *            are still attended to in full, less evenly divided.)
  *   out      device out, [Tq, q_heads, d] of type t; zeros for a query that sees no token
  *   lse      device out or NULL, [Tq, q_heads] float: log of the sum of exp(scale * q.K); -inf where nothing is seen
- * Scores, softmax statistics and sums are fp32; the weights exp(score - max) * v_scale are rounded to fp16 (11 bits, relative to a
- * power of two near the sequence's largest v_scale) for the product with the values.  Results do not depend on the order of
- * workgroups.  What lies in the cache beyond a sequence's length or outside its window has no influence, NaN included.
+ * Scores, softmax statistics and sums are fp32; the weights exp(score) * v_scale are rounded to fp16 for the product with the values: to
+ * 11 bits down to 2^-20 of the largest weight that the query sees, to fewer below that, and to 0 below 2^-31 of it.  (bf16: so for
+ * v_scale from 2^-80 to 2^100; the sums of the softmax lose bits above, weights below.)  Results do not depend on the order of
+ * workgroups.  What lies in the cache beyond a sequence's length or outside a query's window has no influence on its result, NaN included.
  */
 fk_status fk_kv_attend(const fk_kv_cache* cache, const void* q, int64_t q_token_stride, int64_t q_head_stride,
                        int q_heads, int64_t Tq, const int32_t* pages, int max_pages, const int32_t* lens,

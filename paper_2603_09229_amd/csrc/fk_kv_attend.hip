@@ -18,9 +18,11 @@
 // values' in the upper: the address is (byte << 8) + 4 (lane % 32) + 128 for values, one v_perm and an offset in the instruction.  Values
 // are multiplied as fp16 whatever t is (levels are at most 1 or so, 11 bits hold a bf16's 8).
 //
-// The running maximum is only moved when a score passes it by 2^kSlack, the weights' scale (a power of two near the largest s') when one
-// passes that by 2^kScaleSlack: the sums are then multiplied once.  Weights stay below 2^15 and fit fp16; relative to their scale they keep
-// 11 bits, as many as the values have in an uncoded cache of fp16, and sums and statistics are fp32.
+// The exponents' reference m of a row follows its weights 2^(x_j log2 e - m) s'_j rather than its scores: a row's largest weight is put
+// at 2^kTop, and the reference is only moved, and the sums multiplied once, when a weight would pass 2^kFits.  So the weights, which are
+// multiplied as fp16, keep 11 bits, as many as the values have in an uncoded cache of fp16, down to 2^-20 of the row's largest, and
+// vanish below 2^-31 of it, whatever scales other rows see.  The exponentials' sums and the statistics are fp32; where scales are so small
+// that exponentials would pass 2^kMost, weights stay smaller instead.
 //
 // What bounds it.  Single tokens (at most 16 query rows to a cache head): bytes, 2 (d/2 + 2) a token and head.  64 sequences of up to 8192
 // tokens, 8 heads of 128: 353 MB in 83 us, 4.2 TB/s (5.0 where they are equally long; a large copy reaches 5.2); one of 131072: 138 MB in 31 us
@@ -37,8 +39,10 @@
 
 namespace fk {
 
-constexpr float kSlack = 8.f;            // in powers of two
-constexpr float kScaleSlack = 64.f;
+// Weights, in powers of two: the largest after its reference has moved, and at any time.  (The chunk named above: 2^8 1078 us, 2^6 1060, 2^3 1055,
+// since references move less often; each of them drops one more power of two of the smallest weights.)
+constexpr float kTop = 6.f, kFits = 15.5f;
+constexpr float kMost = 96.f, kMostMoved = 90.f;   // the same for the exponentials, of which up to 2^30 are added up
 constexpr float kNone = -3.402823466e38f;   // below every score: the maximum of a row that has seen nothing
 constexpr int kJoinWaves = 8;            // waves of a workgroup that share the rows
 constexpr int kStep = 32;                // tokens a wave takes at a time
@@ -68,14 +72,12 @@ __device__ __forceinline__ uint32_t pk_max_u16(uint32_t a, uint32_t b) {
     return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
 }
 
-// kScaleSlack units as two numbers of type t, at most the largest finite one
-template <bool BF>
-__device__ __forceinline__ uint32_t limit_of(float unit) {
-    const uint32_t l = float_to_lp_any(fminf(kScaleSlack * unit, BF ? 0x1.fep127f : 65504.f), BF);
-    return l | l << 16;
-}
-
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+// x 2^by for by below 0, of which 2^by alone may be too small for 32 bits
+__device__ __forceinline__ float times_exp2(float x, float by) {
+    const float half = exp2_fast(0.5f * by);
+    return x * half * half;
+}
 
 // x / by for any x below 2^32: a multiplication by 2^(32 + s) / by, s = ceil(log2 by), less 2^32
 struct Divider {
@@ -297,13 +299,11 @@ __device__ __forceinline__ float lse_of(float top, float sum) {
     return sum > 0.f || sum != sum ? (top + __log2f(sum)) * 0.6931471805599453f : -INFINITY;
 }
 
-// Maxima, sums and the weights' unit of a wave's rows; a lane keeps its column's, its own tokens' share of the sum.
+// References and sums of a wave's rows; a lane keeps its column's, its own tokens' share of the sum.
 template <int NT, int S>
 struct Softmax {
     float top[NT], sum[NT];    // reference of the exponents (0 before anything is seen), sum of the exponentials
-    float bar[NT];             // a score this much above the reference moves it: any before the first, then kSlack
-    float unit = 0.f, per_unit = 1.f;
-    uint32_t limit2 = 0;       // kScaleSlack units as two numbers of type t
+    float bar[NT];             // a score this much above the reference moves it: any before the first, then kMost
 
     __device__ __forceinline__ Softmax() {
 #pragma unroll
@@ -315,7 +315,8 @@ struct Softmax {
 
     // One step's scores X (before the keys' scales ks, which come times scale log2 e) become weights w; products O move with their
     // reference.  The lane's e-th score is of token first + 16 (e / 4) + e % 4, vs has its values' scales, 16 bits
-    // each, and loses those that must not be multiplied.
+    // each, and loses those that must not be multiplied.  A column's reference depends on what its row sees and on nothing else: other columns'
+    // scores and scales that the row does not see may bring the wave to the branch, but do not move it there.
     template <bool BF>
     __device__ __forceinline__ void step(const floatx4 (&X)[2][NT], const float (&ks)[8], uintx2 (&vs)[2], bool masked,
                                          const Seen<NT>& seen, int first, floatx4 (&O)[S][NT], uintx4 (&w)[NT]) {
@@ -339,48 +340,51 @@ struct Softmax {
                 vs[e / 4][(e & 3) / 2] &= out ? (e & 1 ? 0x0000ffffu : 0xffff0000u) : 0xffffffffu;
             }
         }
-        // The scales against the limit, two at a time as 16-bit integers (they are positive)
+        // The largest of the lane's scales, which are positive and order as 16-bit integers, is below a power of two: scores below `fits`
+        // give weights that fit
         const uint32_t most2 = pk_max_u16(pk_max_u16(vs[0][0], vs[0][1]), pk_max_u16(vs[1][0], vs[1][1]));
-        bool move = pk_max_u16(most2, limit2) != limit2;
+        const uint16_t most = (uint16_t)max(most2 & 0xffffu, most2 >> 16);
+        const float fits = kFits - (float)__builtin_amdgcn_frexp_expf(lp_to_float(most, BF));
+        bool move = false;
 #pragma unroll
         for (int c = 0; c < NT; ++c) {
             peak[c] = x[c][0];
 #pragma unroll
             for (int e = 1; e < 8; ++e) peak[c] = fmaxf(peak[c], x[c][e]);
-            move |= peak[c] > bar[c];
+            move |= peak[c] > fminf(bar[c], fits);
         }
         if (__any(move)) {
-            float ratio = 1.f, most = fmaxf(lp_to_float((uint16_t)most2, BF), lp_to_float((uint16_t)(most2 >> 16), BF));
-            most = fmaxf(most, __shfl_xor(most, 16));
-            most = fmaxf(most, __shfl_xor(most, 32));
-            if (most > kScaleSlack * unit) {                      // the same in all lanes
-                const float to = fminf(__uint_as_float(max(__float_as_uint(most) & 0x7f800000u, 0x00800000u)), 0x1p126f);
-                ratio = unit / to;
-                unit = to;
-                per_unit = 1.f / to;
-                limit2 = limit_of<BF>(to);
-            }
+            uintx2 rare[2] = {vs[0], vs[1]};                      // (scales converted here are not to be kept in registers for below)
+            __asm__("" : "+v"(rare[0]), "+v"(rare[1]));
+            float log_v[8];                                       // (an infinite one makes its weights infinite, not their reference)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) log_v[e] = fminf(__builtin_amdgcn_logf(scale_at<BF>(rare[e / 4], e & 3)), 128.f);
 #pragma unroll
             for (int c = 0; c < NT; ++c) {
-                // (a column's reference moves by its own scores alone: what other rows see has no part in its rounding)
-                float by = fmaxf(peak[c], __shfl_xor(peak[c], 16));
-                by = fmaxf(by, __shfl_xor(by, 32));
-                const bool moves = by > bar[c];
-                by = moves ? by : 0.f;
-                // before anything is seen sum and products are zero, and the first reference may lie anywhere
-                const float shrink = bar[c] == kNone ? 0.f : exp2_fast(-by), f = shrink * ratio;
-                bar[c] = moves ? kSlack : bar[c];
-                top[c] += by;
-                sum[c] *= shrink;
+                float score = peak[c], weight = kNone;
 #pragma unroll
-                for (int s = 0; s < S; ++s) O[s][c] *= f;
+                for (int e = 0; e < 8; ++e) weight = fmaxf(weight, x[c][e] + log_v[e]);
+                score = fmaxf(score, __shfl_xor(score, 16));
+                score = fmaxf(score, __shfl_xor(score, 32));
+                weight = fmaxf(weight, __shfl_xor(weight, 16));
+                weight = fmaxf(weight, __shfl_xor(weight, 32));
+                // before anything is seen sum and products are zero, and the first reference may lie anywhere
+                const bool first = bar[c] == kNone;
+                const bool moves = score > bar[c] || (!first && weight > kFits + 0.01f);   // (a rounding above what brings a lane here)
+                const float by = moves ? fmaxf(weight - kTop, score - kMostMoved) : 0.f;
+                bar[c] = moves ? kMost : bar[c];
+                top[c] += by;
+                sum[c] = first ? 0.f : times_exp2(sum[c], -by);
+                const float shrink = first ? 0.f : exp2_fast(-by);
+#pragma unroll
+                for (int s = 0; s < S; ++s) O[s][c] *= shrink;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[c][e] -= by;
             }
         }
         float v[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = scale_at<BF>(vs[e / 4], e & 3) * per_unit;
+        for (int e = 0; e < 8; ++e) v[e] = scale_at<BF>(vs[e / 4], e & 3);
 #pragma unroll
         for (int c = 0; c < NT; ++c) {
 #pragma unroll
@@ -393,14 +397,12 @@ struct Softmax {
         }
     }
 
-    // The columns' sums, and products in units of the values
-    __device__ __forceinline__ void finish(floatx4 (&O)[S][NT]) {
+    // The columns' sums
+    __device__ __forceinline__ void finish() {
 #pragma unroll
         for (int c = 0; c < NT; ++c) {
             sum[c] += __shfl_xor(sum[c], 16);
             sum[c] += __shfl_xor(sum[c], 32);
-#pragma unroll
-            for (int s = 0; s < S; ++s) O[s][c] *= unit;
         }
     }
 };
@@ -547,7 +549,7 @@ void kv_attend_kernel(AttendArgs A) {
         in.load_values(f, row);
     }
 
-    soft.finish(O);
+    soft.finish();
     float (&top)[NT] = soft.top, (&sum)[NT] = soft.sum;
 
     int last0 = row0;
@@ -609,7 +611,7 @@ void kv_attend_kernel(AttendArgs A) {
             const floatx4 u = tops[(c * 16 + n) * 2], v = tops[(c * 16 + n) * 2 + 1];
             t[c] = fmaxf(fmaxf(fmaxf(u[0], u[1]), fmaxf(u[2], u[3])), fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])));
             const float mine = sum[c] == 0.f ? 0.f : exp2_fast(top[c] - t[c]);
-            if (q == 0) ((float*)(sums + (c * 16 + n) * 2))[wave] = sum[c] * mine;
+            if (q == 0) ((float*)(sums + (c * 16 + n) * 2))[wave] = sum[c] == 0.f ? 0.f : times_exp2(sum[c], top[c] - t[c]);
 #pragma unroll
             for (int s = 0; s < S; ++s) O[s][c] *= mine;
         }
@@ -705,9 +707,8 @@ __global__ __launch_bounds__(64 * WAVES, 4) void kv_join_kernel(AttendArgs A) {
     for (int w = 0; w < WAVES; ++w) t = fmaxf(t, most[w][n]);
 #pragma unroll
     for (int k = 0; k < EACH; ++k) {
-        const float f = exp2_fast(tops[k] - t);
-        factor[k * LANES + wave * 4 + q][n] = f;
-        l += sums[k] * f;
+        factor[k * LANES + wave * 4 + q][n] = exp2_fast(tops[k] - t);
+        l += times_exp2(sums[k], tops[k] - t);
     }
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
