@@ -293,7 +293,7 @@ int fk_stage_timer_stop(double* stage_ms, int* stage_launches);
  *   k_scale, v_scale    [pages, heads, page_size] of type t: the largest magnitude of the row (exact: rows are of type t);
  *                       NaN for a row that holds a value that is not finite, which then reads back as NaN
  *   k_levels, v_levels  [heads, 16] of type t, ascending, finite; in units of the largest magnitude, so within [-1, 1]
- *                       (v_levels: below 65504 in any case, they are multiplied as fp16)
+ *                       (fk_kv_attend multiplies v_levels as fp16: those of bf16 lose bits below 2^-31 of the head's largest)
  * t is FK_F16 or FK_BF16; page_size a power of two from 16 to 65536; d a multiple of 32 up to 256; 1 <= heads <= 256;
  * pages * page_size below 2^40.  A slot is page * page_size + place in the page.  (Levels out of order give other ids, never
  * other memory.)

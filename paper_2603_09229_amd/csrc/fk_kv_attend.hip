@@ -16,7 +16,8 @@
 // Codes become levels two at a time: a byte is the index into a table of 256 pairs of 16-bit levels in LDS, held 32 times, one copy a
 // bank, so that a wave's 64 random indices do not collide.  A row of the table is 256 bytes, the keys' copies in the lower half and the
 // values' in the upper: the address is (byte << 8) + 4 (lane % 32) + 128 for values, one v_perm and an offset in the instruction.  Values
-// are multiplied as fp16 whatever t is (levels are at most 1 or so, 11 bits hold a bf16's 8).
+// are multiplied as fp16 whatever t is; levels of bf16 times the power of two that puts the head's largest at 2^14, so that those down to
+// 2^-31 of it keep their 8 bits, and the products are divided by it at the end.
 //
 // The exponents' reference m of a row follows its weights 2^(x_j log2 e - m) s'_j rather than its scores: a row's largest weight is put
 // at 2^kTop, and the reference is only moved, and the sums multiplied once, when a weight would pass 2^kFits.  So the weights, which are
@@ -240,10 +241,22 @@ struct Table {
     static __device__ __forceinline__ uint16_t level(const KVView& c, int h, int lane) {
         return ((lane & 16) ? c.v_levels : c.k_levels)[h * 16 + (lane & 15)];
     }
-    // A row is sixteen pieces of 16 bytes, eight of the keys and eight of the values.
+    // A row is sixteen pieces of 16 bytes, eight of the keys and eight of the values.  -> what products with the values' levels come times
     template <bool BF, int THREADS>
-    static __device__ __forceinline__ void fill(uint8_t* lds, uint16_t level, int lane) {
-        const uint32_t mine = (lane & 16) ? float_to_half(lp_to_float(level, BF)) : level;
+    static __device__ __forceinline__ float fill(uint8_t* lds, uint16_t level, int lane) {
+        float down = 1.f;
+        uint32_t mine = level;
+        if constexpr (BF) {
+            int top = level & 0x7fff;                             // the largest of 16 lanes: rotated by 8, 4, 2 and 1 (the table waits for it)
+            top = max(top, __builtin_amdgcn_mov_dpp(top, 0x128, 0xf, 0xf, false));
+            top = max(top, __builtin_amdgcn_mov_dpp(top, 0x124, 0xf, 0xf, false));
+            top = max(top, __builtin_amdgcn_mov_dpp(top, 0x122, 0xf, 0xf, false));
+            top = max(top, __builtin_amdgcn_mov_dpp(top, 0x121, 0xf, 0xf, false));
+            // biased exponents: 2^(14 - e) has 127 + 14 - (E - 127)
+            const int up = min(268 - (__builtin_amdgcn_readlane(top, 16) >> 7), 253);
+            down = __uint_as_float((uint32_t)(254 - up) << 23);
+            if (lane & 16) mine = float_to_half(lp_to_float(level, true) * __uint_as_float((uint32_t)up << 23));
+        }
         const int side = lane & 8 ? 16 : 0;
 #pragma unroll 2
         for (int i = 0; i < bytes / 16 / THREADS; ++i) {
@@ -251,6 +264,7 @@ struct Table {
             const uint32_t pair = (uint32_t)__shfl((int)mine, side + (code & 15)) | ((uint32_t)__shfl((int)mine, side + (code >> 4)) << 16);
             ((uintx4*)lds)[at] = uintx4{pair, pair, pair, pair};
         }
+        return down;
     }
 };
 
@@ -397,12 +411,14 @@ struct Softmax {
         }
     }
 
-    // The columns' sums
-    __device__ __forceinline__ void finish() {
+    // The columns' sums, and products with the values' levels as they are
+    __device__ __forceinline__ void finish(floatx4 (&O)[S][NT], float down) {
 #pragma unroll
         for (int c = 0; c < NT; ++c) {
             sum[c] += __shfl_xor(sum[c], 16);
             sum[c] += __shfl_xor(sum[c], 32);
+#pragma unroll
+            for (int s = 0; s < S; ++s) O[s][c] *= down;
         }
     }
 };
@@ -477,7 +493,7 @@ void kv_attend_kernel(AttendArgs A) {
     seen.lo = lo;
     seen.hi = hi;
     load_queries<ND, NT>(A, at, h, row0, n, q, Q, seen);
-    T::fill<BF, THREADS>(lds, level, lane);
+    const float down = T::fill<BF, THREADS>(lds, level, lane);
 
     floatx4 O[S][NT];
     Softmax<NT, S> soft;
@@ -549,7 +565,7 @@ void kv_attend_kernel(AttendArgs A) {
         in.load_values(f, row);
     }
 
-    soft.finish();
+    soft.finish(O, down);
     float (&top)[NT] = soft.top, (&sum)[NT] = soft.sum;
 
     int last0 = row0;

@@ -2,7 +2,7 @@
 of the softmax with hardly any value, rows of zeros.
 
 Tolerance: as in test_gpu_kv_attend.py, and what weights lose that are far below a row's largest.  They are multiplied as fp16, in units in which the row's largest
-weight times scale is at least 2^8; below fp16's smallest normal number each is off by at most 2^-25, so 2^-31 of the largest a token.  The largest one is
+weight times scale is at least 2^6; below fp16's smallest normal number each is off by at most 2^-25, so 2^-31 of the largest a token.  The largest one is
 taken as at most twice the largest channel of the mean of |weight * value| (levels reach 0.6 of a scale and more)."""
 import math
 
@@ -120,5 +120,22 @@ def test_the_range_of_scales_in_bf16(first, later):
     cache.v_scale[table[0, 8:38].long()] *= later
     cache.v_scale[table[1, :2].long()] *= first
     cache.v_scale[table[1, 2:5].long()] *= later
+    got, lse = attend(cache, q, table, lens, starts)
+    check(cache, q, table, lens, starts, 0, got, lse)
+
+
+@pytest.mark.parametrize("t", [F16, BF16])
+@pytest.mark.parametrize("lens,queries,H,G", [([700], [1], 2, 3), ([9000], [2], 1, 4), ([300] * 12, [150] * 12, 8, 3), ([20] * 40, [1] * 40, 8, 2)])
+@pytest.mark.parametrize("largest", [1.0, 2.0 ** -12])
+def test_levels_of_the_values_far_below_the_largest(t, lens, queries, H, G, largest):
+    """A channel whose values are all coded by levels of 3e-6 to 1e-7 of a head's largest keeps them to the type's bits."""
+    P, d = 16, 64
+    if t == F16:
+        largest = 1.0                                             # (levels of 1e-7 are fp16's own smallest numbers)
+    cache, q, table, starts = make(t, lens, queries, H, G, d, P, 47)
+    small = torch.tensor([1.07e-7, 1.3e-6, 2.9e-6, 1.7e-5, 1.1e-4])
+    lv = torch.cat([torch.linspace(-1, -0.2, 5), -small[:3].flip(0), small, torch.tensor([0.3, 0.7, 1.0])]) * largest
+    cache.v_levels.copy_(lv.expand(H, 16).to(t))
+    cache.v_codes[..., 3] = cache.v_codes[..., 3] % 3 + 8 | (cache.v_codes[..., 3] >> 4) % 3 + 5 << 4   # channel 6: above 0; 7: below
     got, lse = attend(cache, q, table, lens, starts)
     check(cache, q, table, lens, starts, 0, got, lse)
