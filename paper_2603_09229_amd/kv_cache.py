@@ -46,6 +46,8 @@ class Server:
     """A batch of sequences over one cache: slots are given out page by page, prompts and steps go through the three calls."""
 
     def __init__(self, k_levels, v_levels, d: int, batch: int, max_len: int, page_size: int = 64):
+        if batch < 1 or max_len < 1:
+            raise ValueError(f"batch and max_len must be positive, got {batch}, {max_len}")
         dev = k_levels.device
         self.max_pages = -(-max_len // page_size)
         self.cache = fk.KVCache.empty(batch * self.max_pages, page_size, k_levels, v_levels, d)
@@ -56,12 +58,22 @@ class Server:
         self.max_len = max_len
 
     def step(self, q, k, v, counts: list[int]) -> torch.Tensor:
-        """counts[b] new tokens of sequence b, one after the other in q [T, q_heads, d], k, v [T, heads, d] -> attention [T, q_heads, d]."""
+        """counts[b] new tokens of sequence b, one after the other in q [T, q_heads, d], k, v [T, heads, d] -> attention [T, q_heads, d].
+
+        Refused before anything changes: counts that are not one for each sequence or not those of the rows, and a sequence that would hold more
+        than max_len tokens (they would have no page, and no angle)."""
+        if len(counts) != len(self.lens) or any(c < 0 for c in counts) or not sum(counts) == len(q) == len(k) == len(v):
+            raise ValueError(f"counts {counts} for {len(self.lens)} sequences and rows of {len(q)}, {len(k)}, {len(v)} tokens")
+        over = [b for b, (held, c) in enumerate(zip(self.lens.tolist(), counts)) if held + c > self.max_len]
+        if over:
+            raise ValueError(f"sequences {over} would hold more than {self.max_len} tokens")
+        if not sum(counts):
+            return torch.empty_like(q)
         dev, P = q.device, self.cache.page_size
         n = torch.tensor(counts, device=dev)
         start = torch.zeros(len(counts) + 1, dtype=torch.int32, device=dev)
         start[1:] = n.cumsum(0)
-        seq = torch.repeat_interleave(torch.arange(len(counts), device=dev), n)
+        seq = torch.repeat_interleave(torch.arange(len(counts), device=dev), n, output_size=len(q))
         pos = self.lens[seq] + torch.arange(len(q), device=dev, dtype=torch.int32) - start[seq]
         slots = self.pages[seq, (pos // P).long()].long() * P + pos % P
         q = fk.fk_kv_append(self.cache, k, v, slots, positions=pos, cos_sin=self.cos_sin, q=q)

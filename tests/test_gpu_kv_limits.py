@@ -1,9 +1,11 @@
-"""fk_kv_attend at the ends of its ranges: windows as long as the type holds, with more queries than tokens.  Inputs, comparison
-and tolerance as in test_gpu_kv_attend.py."""
+"""The 4-bit cache at the ends of its ranges: windows as long as the type holds, with more queries than tokens; sequences that fill their room.
+Inputs, comparison and tolerance as in test_gpu_kv_attend.py."""
 import pytest
 import torch
 
-from tests.test_gpu_kv_attend import BF16, F16, run
+from paper_2603_09229_amd import kv_cache
+from tests import kv_plain
+from tests.test_gpu_kv_attend import BF16, DEV, F16, run
 
 pytestmark = pytest.mark.gpu
 LAST = 2 ** 31 - 1
@@ -17,3 +19,24 @@ def test_the_longest_windows(window, causal):
     run(BF16, [2, 33, 5000], [5, 1, 9], 1, 4, 128, 16, window=window, causal=causal, seed=32)
     run(BF16, [3, 0, 30] * 40, [5, 2, 1] * 40, 3, 2, 96, 16, window=window, causal=causal, seed=33)
     run(F16, [2, 100, 17, 64] * 8, [70, 100, 40, 20] * 8, 8, 3, 128, 16, window=window, causal=causal, seed=34)
+
+
+def test_a_server_fills_its_sequences_to_the_last_token_and_no_further():
+    """max_len is no multiple of the page: the last tokens are turned by their own angles, one more is refused and changes nothing."""
+    g = torch.Generator().manual_seed(35)
+    lv = kv_plain.levels(2, F16, 7, DEV)
+    server = kv_cache.Server(lv, lv, 64, 2, 37, page_size=16)
+    rows = lambda T: [torch.randn(T, h, 64, generator=g).half().to(DEV) for h in (4, 2, 2)]
+    server.step(*rows(66), [36, 30])
+    q, k, v = rows(3)
+    with pytest.raises(ValueError):
+        server.step(q, k, v, [2, 1])
+    assert server.lens.tolist() == [36, 30]
+    out = server.step(q, k, v, [1, 2])
+    assert server.lens.tolist() == [37, 32]
+    pos = torch.tensor([36, 30, 31], device=DEV)
+    cache = server.cache
+    slots = server.pages[torch.tensor([0, 1, 1], device=DEV), pos // 16].long() * 16 + pos % 16
+    want = kv_plain.turned(k, server.cos_sin, pos, False)
+    assert torch.equal(cache.k_scale[slots // 16, :, slots % 16], want.abs().amax(-1))
+    assert server.step(*rows(0), [0, 0]).shape == (0, 4, 64) and out.shape == (3, 4, 64)
