@@ -25,8 +25,13 @@ def learn_levels(rows: torch.Tensor, iters: int = 12) -> torch.Tensor:
     """rows [N, heads, d] (keys as they are cached, so after turning, or values) -> levels [heads, 16], ascending.
 
     One k-means instance a head over all its numbers, each divided by the largest magnitude of its row: N * d points of one feature,
-    16 clusters, which is the shape of the few-cluster pass.  It starts from the 16 even quantiles, so that levels stay in order."""
+    16 clusters, which is the shape of the few-cluster pass.  It starts from the 16 even quantiles, so that levels stay in order.
+    Rows that are not finite are refused: one of them would make all levels of its head NaN."""
     N, H, d = rows.shape
+    if not N:
+        raise ValueError("levels are learned from at least one row")
+    if not rows.isfinite().all():
+        raise ValueError("rows must be finite")
     top = rows.float().abs().amax(dim=-1, keepdim=True)
     x = (rows.float() / torch.where(top > 0, top, 1.0)).to(rows.dtype).transpose(0, 1).reshape(H, N * d, 1).contiguous()
     at = ((torch.arange(16, device=x.device) + 0.5) / 16 * (N * d)).long()

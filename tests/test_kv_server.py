@@ -1,4 +1,4 @@
-"""What kv_cache.Server refuses, before it touches the device: no kernel is launched here and no tensor is on a GPU."""
+"""What kv_cache.Server and learn_levels refuse, before it touches the device: no kernel is launched here and no tensor is on a GPU."""
 import pytest
 import torch
 
@@ -41,3 +41,17 @@ def test_a_step_without_tokens_is_over_at_once():
 def test_no_room_at_all(batch, max_len):
     with pytest.raises(ValueError, match="positive"):
         kv_cache.Server(torch.zeros(1, 16), torch.zeros(1, 16), 64, batch, max_len)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_levels_are_not_learned_from_rows_that_are_not_finite(dtype, bad):
+    rows = torch.randn(50, 2, 32).to(dtype)
+    rows[49, 1, 31] = bad
+    with pytest.raises(ValueError, match="finite"):
+        kv_cache.learn_levels(rows)
+
+
+def test_levels_are_not_learned_from_nothing():
+    with pytest.raises(ValueError, match="at least one row"):
+        kv_cache.learn_levels(torch.zeros(0, 2, 32, dtype=torch.float16))
