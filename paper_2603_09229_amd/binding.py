@@ -303,9 +303,24 @@ class KVCache:
     """A paged key/value cache in 4 bits over the caller's tensors (see fk_kv_cache in include/flashkm.h).
 
     codes [pages, heads, page_size, d/2] uint8, scales [pages, heads, page_size] and levels [heads, 16] of one 16-bit type, the
-    levels ascending.  `KVCache.empty` allocates the codes and scales."""
+    levels ascending.  `KVCache.empty` allocates the codes and scales.  The tensors are attributes of these names; they may be replaced or
+    moved in memory, every call asks where they are."""
+
+    _TENSORS = ("k_codes", "v_codes", "k_scale", "v_scale", "k_levels", "v_levels")
 
     def __init__(self, k_codes, v_codes, k_scale, v_scale, k_levels, v_levels):
+        self.k_codes, self.v_codes, self.k_scale, self.v_scale, self.k_levels, self.v_levels = (
+            k_codes, v_codes, k_scale, v_scale, k_levels, v_levels)
+        self._bind()
+
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        if name in self._TENSORS:
+            object.__setattr__(self, "_at", None)                     # looked at anew by the next call
+
+    def _bind(self):
+        """Checks the tensors and lays down their sizes and places for the library."""
+        k_codes, v_codes, k_scale, v_scale, k_levels, v_levels = tensors = [getattr(self, n) for n in self._TENSORS]
         if k_codes.dim() != 4:
             raise ValueError("k_codes must be [pages, heads, page_size, d/2]")
         P, H, S, half = k_codes.shape
@@ -316,13 +331,19 @@ class KVCache:
         _dev(v_codes, "v_codes", torch.uint8, k_codes.shape)
         _dev(k_scale, "k_scale", t, (P, H, S)); _dev(v_scale, "v_scale", t, (P, H, S))
         _dev(k_levels, "k_levels", t, (H, 16)); _dev(v_levels, "v_levels", t, (H, 16))
-        tensors = (k_codes, v_codes, k_scale, v_scale, k_levels, v_levels)
         if any(x.device != k_codes.device for x in tensors):
             raise ValueError("the cache's tensors must be on one device")
-        self.k_codes, self.v_codes, self.k_scale, self.v_scale, self.k_levels, self.v_levels = tensors
         self.pages, self.heads, self.page_size, self.d, self.dtype, self.device = P, H, S, 2 * half, t, k_codes.device
-        self._struct = _KVCacheStruct(*(x.data_ptr() for x in tensors), P, S, H, 2 * half, _DTYPE[t])
-        self._ref, self._index = ctypes.byref(self._struct), k_codes.get_device()
+        at = tuple(x.data_ptr() for x in tensors)
+        self._struct = _KVCacheStruct(*at, P, S, H, 2 * half, _DTYPE[t])
+        self._ref, self._index, self._at = ctypes.byref(self._struct), k_codes.get_device(), at
+
+    def _here(self):
+        """The struct, with the tensors where they are now."""
+        if self._at != (self.k_codes.data_ptr(), self.v_codes.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr(),
+                        self.k_levels.data_ptr(), self.v_levels.data_ptr()):
+            self._bind()
+        return self._ref
 
     @classmethod
     def empty(cls, pages: int, page_size: int, k_levels, v_levels, d: int) -> "KVCache":
@@ -374,6 +395,7 @@ def _raw_stream(cache: KVCache) -> int:
 def fk_kv_append(cache: KVCache, k, v, slots, *, positions=None, cos_sin=None, interleaved: bool = False, q=None, q_out=None):
     """k, v [T, heads, d] into the slots [T] int64 of the cache, keys turned by the angles of positions [T] int32 (cos_sin
     [max_pos, rot] float32: cosines, then sines); q [T, q_heads, d] is turned likewise and returned (None without q)."""
+    ref = cache._here()
     T, H, d = k.shape[0], cache.heads, cache.d
     kp, kt, kh = _rows(k, "k", cache, T, H)
     vp, vt, vh = _rows(v, "v", cache, T, H)
@@ -392,13 +414,14 @@ def fk_kv_append(cache: KVCache, k, v, slots, *, positions=None, cos_sin=None, i
         heads = q.shape[1]
         qp, qt, qh = _rows(q, "q", cache, T, heads)
         q_out, qo = _result(q_out, "q_out", cache, q, (T, heads, d))
-    _check(lib().fk_kv_append(cache._ref, kp, kt, kh, vp, vt, vh, _array(slots, "slots", cache, torch.int64, (T,)), T, cs, ps,
+    _check(lib().fk_kv_append(ref, kp, kt, kh, vp, vt, vh, _array(slots, "slots", cache, torch.int64, (T,)), T, cs, ps,
                               max_pos, rot, interleaved, qp, qt, qh, heads, qo, _raw_stream(cache)))
     return q_out if q is not None else None
 
 
 def fk_kv_read(cache: KVCache, slots, *, k_out=None, v_out=None):
     """The rows at slots [T] int64 as the values they stand for -> (k, v) [T, heads, d]."""
+    ref = cache._here()
     T = slots.shape[0]
     shape = (T, cache.heads, cache.d)
     if k_out is None:
@@ -407,12 +430,12 @@ def fk_kv_read(cache: KVCache, slots, *, k_out=None, v_out=None):
     else:
         kp = _array(k_out, "k_out", cache, cache.dtype, shape)
     v_out, vp = _result(v_out, "v_out", cache, k_out, shape)
-    _check(lib().fk_kv_read(cache._ref, _array(slots, "slots", cache, torch.int64, (T,)), T, kp, vp, _raw_stream(cache)))
+    _check(lib().fk_kv_read(ref, _array(slots, "slots", cache, torch.int64, (T,)), T, kp, vp, _raw_stream(cache)))
     return k_out, v_out
 
 
 def fk_kv_workspace_bytes(cache: KVCache, B: int, q_heads: int, Tq: int, max_q: int, max_len: int) -> int:
-    return int(lib().fk_kv_workspace_bytes(cache._ref, q_heads, Tq, B, max_q, max_len))
+    return int(lib().fk_kv_workspace_bytes(cache._here(), q_heads, Tq, B, max_q, max_len))
 
 
 def make_kv_workspace(cache: KVCache, B: int, q_heads: int, Tq: int, max_q: int, max_len: int) -> torch.Tensor:
@@ -425,7 +448,7 @@ def make_kv_workspace(cache: KVCache, B: int, q_heads: int, Tq: int, max_q: int,
 def fk_kv_plan(cache: KVCache, B: int, q_heads: int, max_q: int, max_len: int, window: int = 0) -> str:
     """One-line description of what fk_kv_attend would launch for these sizes."""
     buf = ctypes.create_string_buffer(256)
-    _check(lib().fk_kv_plan(cache._ref, q_heads, B, max_q, max_len, window, buf, len(buf)))
+    _check(lib().fk_kv_plan(cache._here(), q_heads, B, max_q, max_len, window, buf, len(buf)))
     return buf.value.decode()
 
 
@@ -434,6 +457,7 @@ def fk_kv_attend(cache: KVCache, q, pages, lens, *, q_start=None, max_q=None, ma
     """q [Tq, q_heads, d] against the cached sequences: pages [B, max_pages] int32, lens [B] int32.  The queries of sequence b are
     q[q_start[b] : q_start[b+1]] (q_start [B+1] int32 with the most of a sequence in max_q; without it max_q each, one by default), the
     last tokens of the sequence.  -> out [Tq, q_heads, d] (and the logarithm of the sums [Tq, q_heads] float32)."""
+    ref = cache._here()
     Tq, heads, _ = q.shape
     qp, qt, qh = _rows(q, "q", cache, Tq, heads)
     B, max_pages = pages.shape
@@ -450,7 +474,7 @@ def fk_kv_attend(cache: KVCache, q, pages, lens, *, q_start=None, max_q=None, ma
         ws = make_kv_workspace(cache, B, heads, Tq, max_q, max_len)
     out, op = _result(out, "out", cache, q, (Tq, heads, cache.d))
     le = torch.empty((Tq, heads), dtype=torch.float32, device=cache.device) if lse else None
-    _check(lib().fk_kv_attend(cache._ref, qp, qt, qh, heads, Tq, _array(pages, "pages", cache, torch.int32, (B, max_pages)), max_pages,
+    _check(lib().fk_kv_attend(ref, qp, qt, qh, heads, Tq, _array(pages, "pages", cache, torch.int32, (B, max_pages)), max_pages,
                               _array(lens, "lens", cache, torch.int32, (B,)), qs, B, max_q, max_len,
                               cache.d ** -0.5 if scale is None else scale, causal, window,
                               op, le.data_ptr() if lse else 0,
