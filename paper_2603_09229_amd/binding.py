@@ -465,7 +465,7 @@ def fk_kv_attend(cache: KVCache, q, pages, lens, *, q_start=None, max_q=None, ma
     if max_q is None:
         if q_start is not None:
             raise ValueError("q_start needs max_q")
-        max_q = max(1, Tq // B)
+        max_q = max(1, Tq // max(1, B))                               # (no sequence: the library refuses it)
     if q_start is not None:
         qs = _array(q_start, "q_start", cache, torch.int32, (B + 1,))
     if not max_len:

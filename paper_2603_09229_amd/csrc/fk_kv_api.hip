@@ -152,7 +152,10 @@ size_t fk_kv_workspace_bytes(const fk_kv_cache* cache, int q_heads, int64_t Tq, 
     KVView c;
     fk_status why;
     if (!view_of(fn, cache, false, &c, &why) || check_queries(fn, c, q_heads, Tq, B, max_q, max_len) != FK_OK) return 0;
-    if (max_len < 1) return 0;
+    if (max_len < 1) {
+        set_error("%s: max_len must be positive", fn);
+        return 0;
+    }
     const size_t n = kv_partial_bytes(choose_kv_plan(c, q_heads, B, max_q, max_len), c.d, c.heads, B);
     return align_up(n, 256) + 256;
 }

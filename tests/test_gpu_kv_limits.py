@@ -3,6 +3,7 @@ Inputs, comparison and tolerance as in test_gpu_kv_attend.py."""
 import pytest
 import torch
 
+from paper_2603_09229_amd import binding as fk
 from paper_2603_09229_amd import kv_cache
 from tests import kv_plain
 from tests.test_gpu_kv_attend import BF16, DEV, F16, run
@@ -40,3 +41,14 @@ def test_a_server_fills_its_sequences_to_the_last_token_and_no_further():
     want = kv_plain.turned(k, server.cos_sin, pos, False)
     assert torch.equal(cache.k_scale[slots // 16, :, slots % 16], want.abs().amax(-1))
     assert server.step(*rows(0), [0, 0]).shape == (0, 4, 64) and out.shape == (3, 4, 64)
+
+
+@pytest.mark.parametrize("B,max_pages", [(0, 3), (0, 0), (1, 0)])
+@pytest.mark.parametrize("own", [False, True])
+def test_no_sequence_and_no_page_are_refused(B, max_pages, own):
+    lv = kv_plain.levels(1, F16, 7, DEV)
+    cache = fk.KVCache.empty(3, 16, lv, lv, 64)
+    pages, lens = torch.zeros(B, max_pages, dtype=torch.int32, device=DEV), torch.zeros(B, dtype=torch.int32, device=DEV)
+    with pytest.raises(fk.FlashKMError, match="positive|max_pages"):
+        fk.fk_kv_attend(cache, torch.zeros(B, 2, 64, dtype=F16, device=DEV), pages, lens,
+                        ws=torch.empty(4096, dtype=torch.uint8, device=DEV) if own else None)

@@ -44,3 +44,12 @@ def test_the_text_is_cut_to_the_buffer():
     assert plan(room=9) == (0, "rows_sha") and plan(room=1) == (0, "")
     assert fk.lib().fk_kv_plan(ctypes.byref(cache()), 32, 1, 1, 100, 0, None, 5) == EINVAL
     assert fk.lib().fk_kv_plan(None, 32, 1, 1, 100, 0, ctypes.create_string_buffer(8), 8) == EINVAL
+
+
+@pytest.mark.parametrize("other,word", [(dict(max_len=0), b"max_len"), (dict(B=0), b"positive"), (dict(max_len=1 << 31), b"max_len")])
+def test_a_workspace_of_nothing_says_why(other, word):
+    fk.lib().fk_kv_read(None, None, 0, None, None, None)              # an error of another call
+    a = dict(heads=32, Tq=1, B=1, max_q=1, max_len=100)
+    a.update(other)
+    assert fk.lib().fk_kv_workspace_bytes(ctypes.byref(cache()), *a.values()) == 0
+    assert b"fk_kv_workspace_bytes" in fk.lib().fk_last_error() and word in fk.lib().fk_last_error()
