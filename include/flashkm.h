@@ -345,6 +345,7 @@ fk_status fk_kv_read(const fk_kv_cache* cache, const int64_t* slots, int64_t T, 
  *   q_start  device, [B+1] int32, ascending from 0: the queries of sequence b are tokens q_start[b] .. q_start[b+1] of q,
  *            at most max_q of them; NULL: max_q each, Tq = B * max_q.  They are the last ones of
  *            the sequence: query i of n sits at position lens[b] - n + i.
+ *   scale    finite, up to 1e38 in magnitude
  *   causal   0: a query sees all tokens of its sequence; otherwise those up to its own position
  *   window   > 0: only tokens less than `window` before its own position; 0: no such limit
  *   max_pages * page_size at most 2^30

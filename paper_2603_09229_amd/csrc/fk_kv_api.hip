@@ -1,4 +1,5 @@
 // C-ABI entry points of the 4-bit key/value cache: argument checks and launches.
+#include <math.h>
 #include <stdio.h>
 
 #include <algorithm>
@@ -197,6 +198,10 @@ fk_status fk_kv_attend(const fk_kv_cache* cache, const void* q, int64_t q_token_
     FK_TRY(check_queries(fn, c, q_heads, Tq, B, max_q, max_len));
     if (max_pages < 1 || window < 0 || (!q_start && Tq != (int64_t)B * max_q)) {
         set_error("%s: max_pages=%d, window=%d, or Tq=%lld without q_start is not B * max_q", fn, max_pages, window, (long long)Tq);
+        return FK_EINVAL;
+    }
+    if (!(fabsf(scale) <= 1e38f)) {                               // (times log2 e it has to be finite)
+        set_error("%s: scale=%g is not a number up to 1e38", fn, (double)scale);
         return FK_EINVAL;
     }
     if ((int64_t)max_pages << c.page_shift > (1 << 30)) {

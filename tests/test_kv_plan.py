@@ -1,11 +1,12 @@
-"""fk_kv_plan: the form, tiles and splits that fk_kv_attend takes, as text, and what it refuses.  No kernel is launched here."""
+"""fk_kv_plan: the form, tiles and splits that fk_kv_attend takes, as text, and what it refuses; what the other calls of the 4-bit cache refuse
+beside test_kv_refusals.py.  No kernel is launched here."""
 import ctypes
 import re
 
 import pytest
 
 from paper_2603_09229_amd import binding as fk
-from tests.test_kv_refusals import EINVAL, EUNSUPPORTED, cache
+from tests.test_kv_refusals import EINVAL, EUNSUPPORTED, attend, cache
 
 
 def plan(c=None, heads=32, B=1, max_q=1, max_len=1000, window=0, room=256):
@@ -53,3 +54,9 @@ def test_a_workspace_of_nothing_says_why(other, word):
     a.update(other)
     assert fk.lib().fk_kv_workspace_bytes(ctypes.byref(cache()), *a.values()) == 0
     assert b"fk_kv_workspace_bytes" in fk.lib().fk_last_error() and word in fk.lib().fk_last_error()
+
+
+@pytest.mark.parametrize("scale", [float("nan"), float("inf"), -float("inf"), 3e38])
+def test_scales_that_are_no_numbers(scale):
+    assert attend(scale=scale, window=0) == EINVAL and b"scale" in fk.lib().fk_last_error()
+    assert attend(scale=-1e38, q=None) == EINVAL and b" q is NULL" in fk.lib().fk_last_error()      # past that check
