@@ -434,7 +434,15 @@ def fk_kv_read(cache: KVCache, slots, *, k_out=None, v_out=None):
     return k_out, v_out
 
 
+def _int32(**values):
+    """ctypes cuts an integer down to the bits that the library takes: what does not fit is refused here."""
+    for name, x in values.items():
+        if not -2 ** 31 <= x < 2 ** 31:
+            raise ValueError(f"{name}={x} is beyond 32 bits")
+
+
 def fk_kv_workspace_bytes(cache: KVCache, B: int, q_heads: int, Tq: int, max_q: int, max_len: int) -> int:
+    _int32(B=B, q_heads=q_heads, max_q=max_q)
     return int(lib().fk_kv_workspace_bytes(cache._here(), q_heads, Tq, B, max_q, max_len))
 
 
@@ -447,7 +455,10 @@ def make_kv_workspace(cache: KVCache, B: int, q_heads: int, Tq: int, max_q: int,
 
 def fk_kv_plan(cache: KVCache, B: int, q_heads: int, max_q: int, max_len: int, window: int = 0) -> str:
     """One-line description of what fk_kv_attend would launch for these sizes."""
+    _int32(B=B, q_heads=q_heads, max_q=max_q)
     buf = ctypes.create_string_buffer(256)
+    window = min(window, 2 ** 31 - 1)                                 # as in fk_kv_attend
+    _int32(window=window)
     _check(lib().fk_kv_plan(cache._here(), q_heads, B, max_q, max_len, window, buf, len(buf)))
     return buf.value.decode()
 
@@ -468,6 +479,9 @@ def fk_kv_attend(cache: KVCache, q, pages, lens, *, q_start=None, max_q=None, ma
         max_q = max(1, Tq // max(1, B))                               # (no sequence: the library refuses it)
     if q_start is not None:
         qs = _array(q_start, "q_start", cache, torch.int32, (B + 1,))
+    if max_q >> 31 or window >> 31:                                   # below 0, which the library refuses, or beyond it
+        window = min(window, 2 ** 31 - 1)                             # (no sequence is that long)
+        _int32(max_q=max_q, window=window)
     if not max_len:
         max_len = max_pages * cache.page_size
     if ws is None:

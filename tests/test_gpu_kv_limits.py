@@ -52,3 +52,28 @@ def test_no_sequence_and_no_page_are_refused(B, max_pages, own):
     with pytest.raises(fk.FlashKMError, match="positive|max_pages"):
         fk.fk_kv_attend(cache, torch.zeros(B, 2, 64, dtype=F16, device=DEV), pages, lens,
                         ws=torch.empty(4096, dtype=torch.uint8, device=DEV) if own else None)
+
+
+def test_integers_beyond_32_bits_are_not_cut():
+    lv = kv_plain.levels(1, F16, 7, DEV)
+    cache = fk.KVCache.empty(3, 16, lv, lv, 64)
+    x = torch.randn(40, 1, 64, device=DEV).half()
+    fk.fk_kv_append(cache, x, x, torch.arange(40, device=DEV))
+    pages, lens = torch.tensor([[0, 1, 2]], dtype=torch.int32, device=DEV), torch.tensor([40], dtype=torch.int32, device=DEV)
+    q, start = x[:4], torch.tensor([0, 4], dtype=torch.int32, device=DEV)
+    want = fk.fk_kv_attend(cache, q, pages, lens, max_q=4)
+    for window in (2 ** 31, 2 ** 32 + 5, 2 ** 40, 10 ** 30):
+        assert torch.equal(fk.fk_kv_attend(cache, q, pages, lens, max_q=4, window=window), want)
+        assert fk.fk_kv_plan(cache, 1, 1, 4, 48, window) == fk.fk_kv_plan(cache, 1, 1, 4, 48)
+    for bad in (2 ** 31, 2 ** 32 + 4, -2 ** 32 + 4):
+        with pytest.raises(ValueError, match="32 bits"):
+            fk.fk_kv_attend(cache, q, pages, lens, q_start=start, max_q=bad)
+        with pytest.raises(ValueError, match="32 bits"):
+            fk.fk_kv_attend(cache, q, pages, lens, max_q=4, window=-2 ** 32 + 4)
+        with pytest.raises(ValueError, match="32 bits"):
+            fk.make_kv_workspace(cache, 1, 1, 4, bad, 48)
+        with pytest.raises(ValueError, match="32 bits"):
+            fk.fk_kv_plan(cache, bad, 1, 4, 48)
+    for other in (dict(max_q=-1, q_start=start), dict(max_q=4, window=-1)):
+        with pytest.raises(fk.FlashKMError):
+            fk.fk_kv_attend(cache, q, pages, lens, **other)
