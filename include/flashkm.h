@@ -363,7 +363,9 @@ fk_status fk_kv_attend(const fk_kv_cache* cache, const void* q, int64_t q_token_
                        const int32_t* q_start, int B, int max_q, int64_t max_len, float scale, int causal, int window,
                        void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
 /* Device bytes that fk_kv_attend needs in ws (256-byte aligned, contents undefined before and after); 0 if unsupported (fk_last_error says
- * why).  Of the cache only the sizes and t are read; max_len >= 1. */
+ * why).  Of the cache only the sizes and t are read; max_len >= 1.  It holds for these B and max_q, and for any shorter max_len or window:
+ * fewer sequences or queries are divided among more workgroups and may need more.  256 (d + 2) bytes for each compute unit and 512 more are
+ * enough for any call, for a program that keeps one workspace while its batch changes. */
 size_t fk_kv_workspace_bytes(const fk_kv_cache* cache, int q_heads, int64_t Tq, int B, int max_q, int64_t max_len);
 /* What fk_kv_attend would launch for these sizes, as fk_plan has it for the other entry points: one line in buf (host memory,
  * NUL-terminated, truncated to buf_bytes).  "rows_shared": the waves of a workgroup share its rows and divide the tokens, `splits`

@@ -447,6 +447,8 @@ def fk_kv_workspace_bytes(cache: KVCache, B: int, q_heads: int, Tq: int, max_q: 
 
 
 def make_kv_workspace(cache: KVCache, B: int, q_heads: int, Tq: int, max_q: int, max_len: int) -> torch.Tensor:
+    """Workspace of fk_kv_attend for these sizes.  Fewer sequences or queries may need more (256 (d + 2) bytes a compute unit and 512
+    are enough for any)."""
     n = fk_kv_workspace_bytes(cache, B, q_heads, Tq, max_q, max_len)
     if n == 0:
         raise FlashKMError(2, f"unsupported attention: {lib().fk_last_error().decode()}")

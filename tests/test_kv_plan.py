@@ -60,3 +60,17 @@ def test_a_workspace_of_nothing_says_why(other, word):
 def test_scales_that_are_no_numbers(scale):
     assert attend(scale=scale, window=0) == EINVAL and b"scale" in fk.lib().fk_last_error()
     assert attend(scale=-1e38, q=None) == EINVAL and b" q is NULL" in fk.lib().fk_last_error()      # past that check
+
+
+@pytest.mark.parametrize("d", range(32, 257, 32))
+def test_one_workspace_is_enough_for_any_call(d):
+    """256 (d + 2) bytes a compute unit (256 of them) and 512; a smaller batch may need more than a larger one."""
+    for H in (1, 3, 8, 64, 256):
+        c = cache(heads=H, d=d)
+        for G in (1, 4, 16, 100):
+            for B in (1, 2, 3, 9, 31, 64, 127, 255, 1000):
+                for max_q in (1, 5, 64, 1000):
+                    for max_len in (1, 700, 5000, 131072, 1 << 30):
+                        assert 0 < fk.lib().fk_kv_workspace_bytes(ctypes.byref(c), H * G, 1, B, max_q, max_len) <= 256 * 256 * (d + 2) + 512
+    need = lambda B: fk.lib().fk_kv_workspace_bytes(ctypes.byref(cache(d=d)), 32, B, B, 1, 8192)
+    assert need(1) > need(64)
