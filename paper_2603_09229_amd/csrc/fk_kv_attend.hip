@@ -791,12 +791,18 @@ KVPlan choose_kv_plan(const KVView& c, int q_heads, int B, int max_q, int64_t re
         p.chunk = cdiv(steps, p.splits) * wg;
         return p;
     }
-    // Many short sequences: a tile to a wave, eight to a workgroup, saves the workgroups' fixed cost and gives up dividing the tokens.  In tenths
-    // of a microsecond, fitted: a round of workgroups that share their rows takes 50 and 8 a step of 256 tokens, one of tiles 42 and 14 a step of
-    // 32.  Measured, one query of 4 heads to each of 8 heads of 128: 64 sequences of 100 tokens 10.2 us shared and 10.5 in tiles, of 200 12.7
-    // and 14.7, 128 of 300 22.8 and 18.3, 110 (9 heads) of up to 9 17.6 and 7.8.
-    const int64_t tiles = cdiv(rows, 16), own = cdiv(B * tiles, 8) * c.heads;
-    const int64_t shared_cost = (50 + 8 * steps) * std::max(blocks, units), own_cost = (42 + 14 * cdiv(reach, kStep)) * std::max(own, units);
+    // Many short sequences: a tile to a wave, eight to a workgroup, saves the workgroups' fixed cost and gives up dividing the tokens.  In tenths of a
+    // microsecond, fitted to 986 measured pairs from 32 to 256 channels, 1 to 4 tiles and 9 to 500 tokens (of which it takes the slower one where that
+    // costs 0.6 % on average, and tiles where they are up to 2 % slower): workgroups that share their rows and hold at most 128 registers run in
+    // pairs on a compute unit, others in rounds; each takes a time of its own and one a step of 256 tokens.  Tiles take theirs a step of 32.
+    // One query of 4 heads to each of 8 heads of 128: 64 sequences of 100 tokens 10.3 us shared and 10.7 in tiles, of 32 9.5 and 6.6; 128 of 300
+    // 23 and 18; of 256 channels 64 of 200 22.6 and 21.5, 32 of 200 12.4 and 21.2.
+    const int64_t tiles = cdiv(rows, 16), own = cdiv(B * tiles, 8) * c.heads, more = std::max(blocks - units, (int64_t)0),
+                  more_own = std::max(own - units, (int64_t)0), w = ND * p.tiles, own_steps = cdiv(reach, kStep);
+    const bool pairs = w <= 2 || (p.tiles == 1 && ND <= 4);
+    const int64_t shared_cost = pairs ? (40 + 5 * w + (4 + 3 * w) * steps) * units + (15 + w + (7 + 2 * w) * steps) * more
+                                      : (60 + 2 * w + (10 + 2 * w) * steps) * cdiv(blocks, units) * units;
+    const int64_t own_cost = (38 + 4 * ND + (7 + 2 * ND) * own_steps) * units + (15 + 9 * ND + (6 + 6 * ND) * own_steps) * more_own;
     if (own_cost < shared_cost) {
         p.join = false;
         p.tiles = 1;
