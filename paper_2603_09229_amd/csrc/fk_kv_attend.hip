@@ -339,25 +339,43 @@ struct Softmax {
         for (int c = 0; c < NT; ++c)
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[c][e] = fmaf(X[e / 4][c][e & 3], ks[e], -top[c]);
+        // The largest of the lane's scales, as 16-bit integers
+        auto largest = [&] {
+            const uint32_t two = pk_max_u16(pk_max_u16(vs[0][0], vs[0][1]), pk_max_u16(vs[1][0], vs[1][1]));
+            return (uint16_t)max(two & 0xffffu, two >> 16);
+        };
+        uint16_t most = largest();
         if (masked) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const int token = first + 16 * (e / 4) + (e & 3);
-                // A scale that is not finite reaches the rows that see it by way of their scores; where none does, or the tokens are
-                // past the end, it may be anything.
-                const float v = scale_at<BF>(vs[e / 4], e & 3);
-                const bool bad = !(v <= 3.402823466e38f), out = bad || token < seen.lo || token >= seen.hi;
 #pragma unroll
                 for (int c = 0; c < NT; ++c)
-                    x[c][e] = token >= seen.hi || token - seen.pos[c] > seen.after || token - seen.pos[c] <= seen.before ? -INFINITY
-                            : bad ? NAN : x[c][e];
-                vs[e / 4][(e & 3) / 2] &= out ? (e & 1 ? 0x0000ffffu : 0xffff0000u) : 0xffffffffu;
+                    x[c][e] = token >= seen.hi || token - seen.pos[c] > seen.after || token - seen.pos[c] <= seen.before ? -INFINITY : x[c][e];
+            }
+            // A value's scale that is not finite goes straight to the sums of the rows that see it, and is not multiplied where none does; past the
+            // end it may be anything, signs included.
+            constexpr uint16_t finite = BF ? 0x7f7f : 0x7bff;
+            if (__any(most > finite)) {
+                uint32_t bad_for = 0;                             // columns of the lane
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int token = first + 16 * (e / 4) + (e & 3);
+                    const bool bad = (vs[e / 4][(e & 3) / 2] >> 16 * (e & 1) & 0x7fffu) > finite, out = bad || token < seen.lo || token >= seen.hi;
+#pragma unroll
+                    for (int c = 0; c < NT; ++c) bad_for |= bad && !(x[c][e] == -INFINITY) ? 1u << c : 0u;
+                    vs[e / 4][(e & 3) / 2] &= out ? (e & 1 ? 0x0000ffffu : 0xffff0000u) : 0xffffffffu;
+                }
+                most = largest();
+                bad_for |= __shfl_xor((int)bad_for, 16);
+                bad_for |= __shfl_xor((int)bad_for, 32);
+#pragma unroll
+                for (int c = 0; c < NT; ++c)
+#pragma unroll
+                    for (int s = 0; s < S; ++s) O[s][c] += bad_for >> c & 1 ? NAN : 0.f;
             }
         }
-        // The largest of the lane's scales, which are positive and order as 16-bit integers, is below a power of two: scores below `fits`
-        // give weights that fit
-        const uint32_t most2 = pk_max_u16(pk_max_u16(vs[0][0], vs[0][1]), pk_max_u16(vs[1][0], vs[1][1]));
-        const uint16_t most = (uint16_t)max(most2 & 0xffffu, most2 >> 16);
+        // Scales are positive and order as integers, the largest is below a power of two: scores below `fits` give weights that fit
         const float fits = kFits - (float)__builtin_amdgcn_frexp_expf(lp_to_float(most, BF));
         bool move = false;
 #pragma unroll
@@ -370,9 +388,12 @@ struct Softmax {
         if (__any(move)) {
             uintx2 rare[2] = {vs[0], vs[1]};                      // (scales converted here are not to be kept in registers for below)
             __asm__("" : "+v"(rare[0]), "+v"(rare[1]));
-            float log_v[8];                                       // (an infinite one makes its weights infinite, not their reference)
+            float log_v[8];                                       // (one that is not finite has its part in the products, not in the reference)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) log_v[e] = fminf(__builtin_amdgcn_logf(scale_at<BF>(rare[e / 4], e & 3)), 128.f);
+            for (int e = 0; e < 8; ++e) {
+                const float v = scale_at<BF>(rare[e / 4], e & 3);
+                log_v[e] = v <= 3.402823466e38f ? __builtin_amdgcn_logf(v) : -INFINITY;
+            }
 #pragma unroll
             for (int c = 0; c < NT; ++c) {
                 float score = peak[c], weight = kNone;

@@ -6,7 +6,7 @@ import torch
 from paper_2603_09229_amd import binding as fk
 from paper_2603_09229_amd import kv_cache
 from tests import kv_plain
-from tests.test_gpu_kv_attend import BF16, DEV, F16, run
+from tests.test_gpu_kv_attend import BF16, DEV, F16, make, run
 
 pytestmark = pytest.mark.gpu
 LAST = 2 ** 31 - 1
@@ -77,3 +77,48 @@ def test_integers_beyond_32_bits_are_not_cut():
     for other in (dict(max_q=-1, q_start=start), dict(max_q=4, window=-1)):
         with pytest.raises(fk.FlashKMError):
             fk.fk_kv_attend(cache, q, pages, lens, **other)
+
+
+@pytest.mark.parametrize("t", [F16, BF16])
+@pytest.mark.parametrize("lens,queries,H,G", [([300], [40], 1, 2), ([9000], [6], 1, 4), ([300, 170] * 6, [200, 170] * 6, 8, 3), ([90, 40] * 16, [40, 40] * 16, 8, 3)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_a_value_that_is_not_finite_leaves_the_softmax_alone(t, lens, queries, H, G, bad):
+    """Rows that see it give no number, others the same bits; the logarithm of the sum is a matter of the keys, wherever in a step the token lies."""
+    cache, q, table, starts = make(t, lens, queries, H, G, 64, 16, 51)
+    at = [L - n // 2 for L, n in zip(lens, queries)]                    # among the queries
+    call = lambda: fk.fk_kv_attend(cache, q, table, torch.tensor(lens, dtype=torch.int32, device=DEV), max_q=max(queries), max_len=max(lens), lse=True,
+                                   q_start=torch.tensor(starts, dtype=torch.int32, device=DEV))
+    clean, clean_lse = call()
+    for places in (at, [5] * len(lens)):
+        was = cache.v_scale.clone()
+        for b, p in enumerate(places):
+            cache.v_scale[table[b, p // 16].long(), :, p % 16] = bad
+        got, lse = call()
+        cache.v_scale.copy_(was)
+        for b, (L, n) in enumerate(zip(lens, queries)):
+            sees = L - n + torch.arange(n, device=DEV) >= places[b]
+            s = slice(starts[b], starts[b + 1])
+            assert not got[s][sees].isfinite().any() and torch.equal(got[s][~sees], clean[s][~sees]) and torch.equal(lse[s][~sees], clean_lse[s][~sees])
+        # (another reference rounds it otherwise: two sums of fp32 numbers, none negative)
+        assert ((lse - clean_lse).abs() <= 2.0 ** -20 * (1 + clean_lse.abs())).all()
+
+
+@pytest.mark.parametrize("t", [F16, BF16])
+@pytest.mark.parametrize("lens,queries,H,G", [([301, 7], [1, 1], 2, 4), ([9003], [6], 1, 4), ([305, 171] * 6, [200, 170] * 6, 8, 3), ([91, 44] * 16, [40, 40] * 16, 8, 3)])
+@pytest.mark.parametrize("window", [0, 30])
+def test_what_no_query_sees_may_be_anything(t, lens, queries, H, G, window):
+    """Past the end, in pages of nobody and before every window: numbers of either sign, infinities and NaN, mixed or all alike, give the same bits."""
+    cache, q, table, starts = make(t, lens, queries, H, G, 64, 16, 52, window=window)
+    call = lambda: fk.fk_kv_attend(cache, q, table, torch.tensor(lens, dtype=torch.int32, device=DEV), max_q=max(queries), max_len=max(lens), lse=True,
+                                   q_start=torch.tensor(starts, dtype=torch.int32, device=DEV), window=window)
+    free = cache.v_scale.isnan()                                        # as make() leaves them
+    want, want_lse = call()
+    assert want.isfinite().all()
+    big = torch.finfo(t).max
+    mixed = torch.tensor([-1e-4, float("inf"), -big, 0.0, -float("inf"), big, -0.0, float("nan"), 1e-6], device=DEV).to(t)
+    for fill in [mixed] + [mixed[i:i + 1] for i in range(len(mixed))]:
+        for scale in (cache.k_scale, cache.v_scale):
+            n = int(free.sum())
+            scale[free] = fill.repeat(-(-n // len(fill)))[:n]
+        got, lse = call()
+        assert torch.equal(got, want) and torch.equal(lse, want_lse)
