@@ -304,7 +304,9 @@ class KVCache:
 
     codes [pages, heads, page_size, d/2] uint8, scales [pages, heads, page_size] and levels [heads, 16] of one 16-bit type, the
     levels ascending.  `KVCache.empty` allocates the codes and scales.  The tensors are attributes of these names; they may be replaced or
-    moved in memory, every call asks where they are."""
+    moved in memory, every call asks where they are.
+
+    The cache is for inference: results of fk_kv_append, fk_kv_read and fk_kv_attend carry no gradient, whether their inputs ask for one or not."""
 
     _TENSORS = ("k_codes", "v_codes", "k_scale", "v_scale", "k_levels", "v_levels")
 

@@ -26,7 +26,8 @@ def learn_levels(rows: torch.Tensor, iters: int = 12) -> torch.Tensor:
 
     One k-means instance a head over all its numbers, each divided by the largest magnitude of its row: N * d points of one feature,
     16 clusters, which is the shape of the few-cluster pass.  It starts from the 16 even quantiles, so that levels stay in order.
-    Rows that are not finite are refused: one of them would make all levels of its head NaN."""
+    Rows that are not finite are refused: one of them would make all levels of its head NaN.  No gradient goes through a fit."""
+    rows = rows.detach()
     N, H, d = rows.shape
     if not N:
         raise ValueError("levels are learned from at least one row")

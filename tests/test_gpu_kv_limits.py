@@ -122,3 +122,14 @@ def test_what_no_query_sees_may_be_anything(t, lens, queries, H, G, window):
             scale[free] = fill.repeat(-(-n // len(fill)))[:n]
         got, lse = call()
         assert torch.equal(got, want) and torch.equal(lse, want_lse)
+
+
+def test_nothing_carries_a_gradient():
+    """Inputs that ask for one: results do not, and learned levels are those of the same rows (not the first guess with a gradient of its own)."""
+    rows = torch.randn(40, 2, 64, device=DEV, generator=torch.Generator(DEV).manual_seed(5)).half()
+    lv = kv_cache.learn_levels(rows)
+    asking = rows.clone().requires_grad_()
+    got = kv_cache.learn_levels(asking)
+    assert not got.requires_grad and torch.equal(got, lv)
+    server = kv_cache.Server(lv, lv, 64, 1, 64)
+    assert not server.step(asking, asking, asking, [40]).requires_grad
