@@ -26,13 +26,13 @@
 // that exponentials would pass 2^kMost, weights stay smaller instead.
 //
 // What bounds it.  Single tokens (at most 16 query rows to a cache head): bytes, 2 (d/2 + 2) a token and head.  64 sequences of up to 8192
-// tokens, 8 heads of 128: 353 MB in 83 us, 4.2 TB/s (5.0 where they are equally long; a large copy reaches 5.2); one of 131072: 138 MB in 31 us
-// and the join 4.7.  Few tokens: a workgroup's fixed cost, about 6 us with its launch, of which the chain of first loads (page, codes; the length
+// tokens, 8 heads of 128: 353 MB in 83 us, 4.2 TB/s (5.0 where they are equally long; a large copy reaches 5.2); one of 131072: 138 MB in 31
+// to 34 us and the join 4.9.  Few tokens: a workgroup's fixed cost, about 6 us with its launch, of which the chain of first loads (page, codes; the length
 // is not waited for), the table (64 KiB of LDS) and the exchange between the waves are a third each, then 1.1 us a step of 8 x 32 tokens.
-// Many sequences of few tokens share workgroups, a wave each: 110 of up to 9, 9 heads, 7.8 us.
+// Many sequences of few tokens share workgroups, a wave each: 110 of up to 9, 9 heads, 7.6 us.
 // Many rows: vector instructions.  A step of 48 rows and 32 tokens at d = 128 takes 48 MFMA (768 cycles), 64 lookups and about 240 vector
 // instructions with 24 exponentials (1340 cycles); two waves a SIMD overlap a third of the two.  Two sequences of 4096 queries over up to
-// 9000 tokens, 32 query heads: 852 GFLOP in 1042 to 1066 us, 0.8 PFLOP/s; a large product of the library reaches 1.2 on this card.
+// 9000 tokens, 32 query heads: 852 GFLOP in 1058 us, 0.8 PFLOP/s (the first 30 passes of a program 1130); a large product of the library reaches 1.2 on this card.
 #include <algorithm>
 
 #include "fk_device.h"
@@ -778,8 +778,8 @@ __global__ __launch_bounds__(64 * WAVES, 4) void kv_join_kernel(AttendArgs A) {
 }
 
 // Most tiles of a wave: as many as leave room for two waves a SIMD without spills (O takes 8 registers a tile and 32 channels, q 4).  With
-// one more, 2 sequences of 1024 queries over 4096 tokens, 16 query heads: d = 256 two tiles 495 us, one 232; d = 224 395 and 226.  With
-// one less: d = 128 chunk as above two tiles 1245 us, three 1220, when they were measured.
+// one more, 2 sequences of 1024 queries over 4096 tokens, 16 query heads: d = 256 two tiles 462 us, one 246; d = 224 337 and 238.  With
+// one less: d = 128 chunk as above two tiles 1176 us, three 1054.
 static constexpr int own_tiles(int ND) { return ND <= 2 ? 4 : ND <= 4 ? 3 : ND <= 6 ? 2 : 1; }
 static constexpr int join_tiles(int ND) { return ND <= 2 ? 4 : ND <= 4 ? 3 : ND <= 6 ? 2 : 1; }
 
@@ -790,7 +790,7 @@ KVPlan choose_kv_plan(const KVView& c, int q_heads, int B, int max_q, int64_t re
     p.splits = 1;
     p.chunk = INT32_MAX / 2;
     // Waves with rows of their own need no exchange at the end, but the rows' workgroups alone have to fill the chip (8 x 5 queries of 16
-    // heads of 256 over 4000 tokens: 16 workgroups 360 us, divided by tokens too 22); otherwise the tokens are divided.
+    // heads of 256 over 4000 tokens: 16 workgroups 235 us, divided by tokens too 23); otherwise the tokens are divided.
     const int64_t own_blocks = (int64_t)B * c.heads * cdiv(rows, 16 * own_tiles(ND) * own_waves(own_tiles(ND)));
     if (rows > 16 * join_tiles(ND) && own_blocks >= units) {
         p.join = false;
@@ -801,11 +801,11 @@ KVPlan choose_kv_plan(const KVView& c, int q_heads, int B, int max_q, int64_t re
     p.join = true;
     p.tiles = (int)std::min(cdiv(rows, 16), (int64_t)join_tiles(ND));
     p.row_blocks = (int)cdiv(rows, 16 * p.tiles);
-    // One workgroup to a compute unit: 8 heads, one sequence of 131072 tokens 64 splits 40.6 us, 32 37.8, 24 43.7.
+    // One workgroup to a compute unit: 8 heads, one sequence of 131072 tokens 64 splits 38.2 us, 32 35.6, 24 41.4.
     const int64_t wg = kJoinWaves * kStep, blocks = (int64_t)B * c.heads * p.row_blocks;
     const int64_t want = blocks >= units ? 1 : units / blocks, steps = cdiv(reach, wg);
-    // Splitting costs the second launch, about four steps of a workgroup: 8 heads of 128, one sequence of 700 tokens (3 steps) 10.6 us
-    // in one piece and 11.1 in three, of 1500 (6) 14.7 and 11.9 in six; 24 sequences of 2048 (8), 4 heads of 64, 13.5 and 13.9 in two.
+    // Splitting costs the second launch, about four steps of a workgroup: 8 heads of 128, one sequence of 700 tokens (3 steps) 10.1 us
+    // in one piece and 10.0 in three, of 1500 (6) 13.8 and 10.4 in six; 24 sequences of 2048 (8), 4 heads of 64, 13.3 and 13.0 in two.
     p.splits = (int)std::min({want, steps, (int64_t)kMostSplits});
     if (steps - cdiv(steps, p.splits) <= 4) p.splits = 1;
     if (p.splits > 1) {

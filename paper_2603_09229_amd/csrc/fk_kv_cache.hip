@@ -7,8 +7,9 @@
 //
 // A row is held by L lanes of a wave, 8 channels (16 bytes) each, so that rows of 64 / L heads move together.
 //
-// What bounds it: bytes for many tokens (16384 of 8 + 8 + 32 rows of 128: 361 MB in 76 us, 4.7 TB/s, where a large copy reaches 5.2; reading
-// 20000 tokens of 8 + 8 rows of 128: 103 MB in 24 us, 4.3), the launch and three dependent loads for few (3.9 and 2.1 us for one token).
+// What bounds it: bytes for many tokens (16384 of 8 + 8 + 32 rows of 128: 361 MB in 74 us one call after the other, 80 by the profiler, 4.9 and 4.5 TB/s,
+// where a large copy reaches 5.2; reading 20000 tokens of 8 + 8 rows of 128: 103 MB in 23 us, 4.5), the launch and three dependent loads for
+// few (3.8 and 2.1 us for one token), the latency of one round of workgroups between (4099 tokens of 4 + 4 + 24 rows of 64: 13 us).
 #include "fk_device.h"
 #include "fk_kv.h"
 
@@ -217,7 +218,7 @@ __global__ __launch_bounds__(kAppendThreads) void kv_read_kernel(KVView c, const
 static int lanes_of(int d) { return d <= 32 ? 4 : d <= 64 ? 8 : d <= 128 ? 16 : 32; }
 
 // Waves for all units, but no more workgroups than the chip holds at once (`each` to a compute unit): the rest is done in turns, so that
-// the levels are loaded once.  16384 tokens of 8 + 8 + 32 rows of 128: 6 to a unit 86 us, 8 (of which 6 run first, then 2) 100.
+// the levels are loaded once.  16384 tokens of 8 + 8 + 32 rows of 128: 6 to a unit 74 us, 8 (of which 6 run first, then 2) 81.
 static unsigned grid_for(int64_t units, int each) {
     const int64_t blocks = cdiv(units, kAppendThreads / 64), most = (int64_t)device_cu_count() * each;
     return (unsigned)(blocks < most ? blocks : most);
