@@ -299,6 +299,13 @@ def fk_standard_update(X, assign, C_prev_f32, *, sums=None):
     return C_out, counts
 
 
+def _int32(**values):
+    """ctypes cuts an integer down to the bits that the library takes: what does not fit is refused here."""
+    for name, x in values.items():
+        if not -2 ** 31 <= x < 2 ** 31:
+            raise ValueError(f"{name}={x} is beyond 32 bits")
+
+
 class KVCache:
     """A paged key/value cache in 4 bits over the caller's tensors (see fk_kv_cache in include/flashkm.h).
 
@@ -326,6 +333,7 @@ class KVCache:
         if k_codes.dim() != 4:
             raise ValueError("k_codes must be [pages, heads, page_size, d/2]")
         P, H, S, half = k_codes.shape
+        _int32(page_size=S, heads=H, d=2 * half)
         t = k_scale.dtype
         if t not in _DTYPE:
             raise ValueError(f"k_scale must be a type of the library, got {t}")
@@ -434,13 +442,6 @@ def fk_kv_read(cache: KVCache, slots, *, k_out=None, v_out=None):
     v_out, vp = _result(v_out, "v_out", cache, k_out, shape)
     _check(lib().fk_kv_read(ref, _array(slots, "slots", cache, torch.int64, (T,)), T, kp, vp, _raw_stream(cache)))
     return k_out, v_out
-
-
-def _int32(**values):
-    """ctypes cuts an integer down to the bits that the library takes: what does not fit is refused here."""
-    for name, x in values.items():
-        if not -2 ** 31 <= x < 2 ** 31:
-            raise ValueError(f"{name}={x} is beyond 32 bits")
 
 
 def fk_kv_workspace_bytes(cache: KVCache, B: int, q_heads: int, Tq: int, max_q: int, max_len: int) -> int:

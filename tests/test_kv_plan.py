@@ -4,6 +4,7 @@ import ctypes
 import re
 
 import pytest
+import torch
 
 from paper_2603_09229_amd import binding as fk
 from tests.test_kv_refusals import EINVAL, EUNSUPPORTED, attend, cache
@@ -74,3 +75,11 @@ def test_one_workspace_is_enough_for_any_call(d):
                         assert 0 < fk.lib().fk_kv_workspace_bytes(ctypes.byref(c), H * G, 1, B, max_q, max_len) <= 256 * 256 * (d + 2) + 512
     need = lambda B: fk.lib().fk_kv_workspace_bytes(ctypes.byref(cache(d=d)), 32, B, B, 1, 8192)
     assert need(1) > need(64)
+
+
+def test_a_page_beyond_32_bits_is_not_cut():
+    """2^32 + 64 tokens a page are not a page of 64 (sizes alone: nothing is allocated)."""
+    codes, scale = torch.empty(1, 1, 2 ** 32 + 64, 16, dtype=torch.uint8, device="meta"), torch.empty(1, 1, 2 ** 32 + 64, dtype=torch.float16, device="meta")
+    levels = torch.empty(1, 16, dtype=torch.float16, device="meta")
+    with pytest.raises(ValueError, match="page_size=4294967360 is beyond 32 bits"):
+        fk.KVCache(codes, codes, scale, scale, levels, levels)
