@@ -4,6 +4,8 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 from pathlib import Path
 
 PKG = Path(__file__).resolve().parent
@@ -31,22 +33,32 @@ def sources() -> list[Path]:
 
 
 def build(verbose: bool = True) -> Path:
-    """Always recompiles (a few tens of seconds); raises on any compiler error."""
-    tmp = LIB.with_suffix(f".tmp{os.getpid()}.so")
-    cmd = [HIPCC, *FLAGS, "-o", str(tmp), *map(str, sources()), *LIBS]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    proc = subprocess.run(cmd, capture_output=True, text=True)
-    # the host pass warns that it does not know the packed-fp32 feature: harmless
-    noise = "is not a recognized feature for this target"
-    err = "\n".join(l for l in proc.stderr.splitlines() if noise not in l)
-    if verbose and err.strip():
-        print(err, file=sys.stderr)
-    if proc.returncode != 0:
-        if tmp.exists():
-            tmp.unlink()
-        raise RuntimeError(f"hipcc failed ({proc.returncode}):\n{err}")
-    os.replace(tmp, LIB)
+    """Always recompiles, one compiler a source on the machine's processors; raises on any compiler error."""
+    with tempfile.TemporaryDirectory(dir=PKG, prefix=".build") as tmp:
+        def run(cmd):
+            if verbose:
+                print(" ".join(cmd), flush=True)
+            proc = subprocess.run(cmd, capture_output=True, text=True)
+            # the host pass warns that it does not know the packed-fp32 feature: harmless
+            noise = "is not a recognized feature for this target"
+            err = "\n".join(l for l in proc.stderr.splitlines() if noise not in l)
+            if verbose and err.strip():
+                print(err, file=sys.stderr)
+            if proc.returncode != 0:
+                raise RuntimeError(f"hipcc failed ({proc.returncode}):\n{err}")
+
+        # the longest first, with the headers they include: what is left at the end is short
+        def length(source):
+            text = source.read_text()
+            return len(text) + sum(h.stat().st_size for h in CSRC.glob("*.h") if f'"{h.name}"' in text)
+
+        todo = sorted(sources(), key=length, reverse=True)
+        objects = [str(Path(tmp) / (s.name + ".o")) for s in todo]
+        with ThreadPoolExecutor(min(8, os.cpu_count() or 1)) as pool:
+            list(pool.map(lambda so: run([HIPCC, *(f for f in FLAGS if f != "-shared"), "-c", "-o", so[1], str(so[0])]), zip(todo, objects)))
+        made = str(Path(tmp) / LIB.name)
+        run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", made, *objects, *LIBS])
+        os.replace(made, LIB)
     return LIB
 
 
