@@ -374,6 +374,72 @@ size_t fk_kv_workspace_bytes(const fk_kv_cache* cache, int q_heads, int64_t Tq, 
  * Host-only; of the cache only the sizes and t are read; max_len >= 1. */
 int fk_kv_plan(const fk_kv_cache* cache, int q_heads, int B, int max_q, int64_t max_len, int window, char* buf, size_t buf_bytes);
 
+/*
+ * fk_kv_attend for a tree of drafted tokens: the n queries of a sequence are its last n tokens, at places lens[b] - n + j, and each sees
+ * what lies before the tree and those tokens of the tree that its mask marks.  Arguments as for fk_kv_attend, but for
+ *   tree     device, [Tq, words] uint64: bit j % 64 of word j / 64 of a query's row says that it sees token j of its sequence's n.  Any
+ *            mask will do: for the tree of a draft a row has the token itself and its ancestors.  Bits from n on are ignored.
+ *   words    of a row; 64 * words >= max_q, Tq * words < 2^29
+ *   window   > 0: of the tokens that a query would see, in the order of their places, only the last `window`; 0: no such limit
+ * A row that sees nothing gives 0 and lse -inf.  The workspace is that of fk_kv_attend for these sizes.
+ */
+fk_status fk_kv_attend_tree(const fk_kv_cache* cache, const void* q, int64_t q_token_stride, int64_t q_head_stride,
+                            int q_heads, int64_t Tq, const int32_t* pages, int max_pages, const int32_t* lens,
+                            const int32_t* q_start, int B, int max_q, int64_t max_len, float scale, int window,
+                            const uint64_t* tree, int words, void* out, float* lse, void* ws, size_t ws_bytes,
+                            void* stream);
+
+/*
+ * Attention weights added up over queries, a number a token and cache head: what eviction goes by.
+ *   mass_out = (place < known[b] ? decay * mass : 0) + sum of exp(scale * q.k - lse) over the queries of the sequence and the heads of the
+ *   group that see the token
+ * for every place of [0, lens[b]) and every cache head; other places are left as they are.
+ *   mass, mass_out   device, [pages, heads, page_size] float, as the cache's scales lie; they may be one tensor, otherwise they do not overlap.
+ *   lse              device, [Tq, q_heads] float, as fk_kv_attend gives it for these queries; a row with -inf adds nothing
+ *   known            device, [B] int32, or NULL: tokens from place known[b] on have no weights yet, and what mass holds of them is not
+ *                    read.  lens[b] less the new tokens for a decoding step, 0 for a prompt; NULL: all have.
+ *   decay            finite; 1 adds up, less than 1 lets older weights fade
+ * The other arguments are those of fk_kv_attend; the keys of the cache are read, its values are not.  No sum depends on the order of
+ * workgroups.  A page belongs to one sequence of a call (two would write its weights at once).  A key that is not finite has the weight NaN if a query sees it.
+ */
+fk_status fk_kv_weigh(const fk_kv_cache* cache, const void* q, int64_t q_token_stride, int64_t q_head_stride, int q_heads,
+                      int64_t Tq, const float* lse, const int32_t* pages, int max_pages, const int32_t* lens,
+                      const int32_t* q_start, int B, int max_q, int64_t max_len, float scale, int causal, int window,
+                      const int32_t* known, float decay, const float* mass, float* mass_out, void* stream);
+
+/*
+ * The places that stay when a sequence of more than `keep` tokens is cut down to `keep`: its first `first` ones, its last `last` ones, and of the
+ * others those with the largest weights, each head its own.  Of equal weights the lower place stays; NaN is below every number.
+ *   mass     device, [pages, heads, page_size] float
+ *   pages, lens, max_len   as for fk_kv_attend
+ *   keep     >= 1, first + last <= keep
+ *   kept     device out, [B, heads, keep] int32: the places in ascending order, -1 behind them; all of a sequence of up to `keep` tokens
+ *   counts   device out, [B] int32: min(lens, keep)
+ *   ws       device, fk_kv_choose_workspace_bytes(...) bytes, 256-byte aligned, contents undefined before and after; NULL if that is 0
+ */
+fk_status fk_kv_choose(const fk_kv_cache* cache, const float* mass, const int32_t* pages, int max_pages, const int32_t* lens,
+                       int B, int64_t max_len, int keep, int first, int last, int32_t* kept, int32_t* counts, void* ws,
+                       size_t ws_bytes, void* stream);
+size_t fk_kv_choose_workspace_bytes(const fk_kv_cache* cache, int B, int64_t max_len);
+
+/*
+ * Rows moved to the front of their sequences: for j < counts[b], place start[b] + j of sequence b gets, in each head, the row of place
+ * start[b] + kept[b, h, j]; keys, values and their scales, bit by bit.
+ *   pages      device, [B, max_pages] int32: the sequences' pages
+ *   kept       device, [B, kept_heads, max_kept] int32; kept_heads 1 (the same places for all heads) or cache->heads
+ *   counts     device, [B] int32 (at most max_kept count)
+ *   start      device, [B] int32, or NULL: 0
+ *   to_pages   device, [B, to_max_pages] int32: where the rows go, or NULL or `pages`: in place.  In place kept[b, h] ascends (no place twice), so
+ *              that no row moves back; other pages have none in common with those that are read.  No page is written for two sequences.
+ *   mass       device, [pages, heads, page_size] float, or NULL: weights that move with their rows
+ * Cutting down to the places of fk_kv_choose has start = NULL; an accepted branch of a drafted tree has the number of tokens before the tree in
+ * start and the branch's tokens, counted within the tree, in kept.  The sequence's length is then start + counts.  A row whose place is
+ * negative or outside the table, or whose page is outside the cache, is left out.
+ */
+fk_status fk_kv_compact(const fk_kv_cache* cache, const int32_t* pages, int max_pages, const int32_t* kept, int kept_heads,
+                        int max_kept, const int32_t* counts, const int32_t* start, const int32_t* to_pages,
+                        int to_max_pages, int B, float* mass, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

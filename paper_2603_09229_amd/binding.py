@@ -23,7 +23,8 @@ EXPORTS = ("fk_last_error", "fk_workspace_bytes", "fk_assign", "fk_sort_inverse"
            "fk_lloyd_iter", "fk_lloyd_ooc", "fk_ooc_workspace_bytes", "fk_stage_timer_start",
            "fk_stage_timer_stop", "fk_plan", "fk_set_option", "fk_standard_assign",
            "fk_standard_update", "fk_assign_static", "fk_assign_static_limit", "fk_kv_append", "fk_kv_read",
-           "fk_kv_attend", "fk_kv_workspace_bytes", "fk_kv_plan")
+           "fk_kv_attend", "fk_kv_workspace_bytes", "fk_kv_plan", "fk_kv_attend_tree", "fk_kv_weigh", "fk_kv_choose",
+           "fk_kv_choose_workspace_bytes", "fk_kv_compact")
 STAGES = ("assign", "sort", "reduce", "finalize")
 
 
@@ -85,6 +86,17 @@ def lib() -> ctypes.CDLL:
                                    vp, sz, vp]
         L.fk_kv_workspace_bytes.restype = sz
         L.fk_kv_workspace_bytes.argtypes = [cache, i32, i64, i32, i32, i64]
+        f32 = ctypes.c_float
+        L.fk_kv_attend_tree.restype = i32
+        L.fk_kv_attend_tree.argtypes = [cache, vp, i64, i64, i32, i64, vp, i32, vp, vp, i32, i32, i64, f32, i32, vp, i32, vp, vp, vp, sz, vp]
+        L.fk_kv_weigh.restype = i32
+        L.fk_kv_weigh.argtypes = [cache, vp, i64, i64, i32, i64, vp, vp, i32, vp, vp, i32, i32, i64, f32, i32, i32, vp, f32, vp, vp, vp]
+        L.fk_kv_choose.restype = i32
+        L.fk_kv_choose.argtypes = [cache, vp, vp, i32, vp, i32, i64, i32, i32, i32, vp, vp, vp, sz, vp]
+        L.fk_kv_choose_workspace_bytes.restype = sz
+        L.fk_kv_choose_workspace_bytes.argtypes = [cache, i32, i64]
+        L.fk_kv_compact.restype = i32
+        L.fk_kv_compact.argtypes = [cache, vp, i32, vp, i32, i32, vp, vp, vp, i32, i32, vp, vp]
         L.fk_kv_plan.restype = i32
         L.fk_kv_plan.argtypes = [cache, i32, i32, i32, i64, i32, ctypes.c_char_p, sz]
         L.fk_plan.restype = i32
@@ -468,6 +480,22 @@ def fk_kv_plan(cache: KVCache, B: int, q_heads: int, max_q: int, max_len: int, w
     return buf.value.decode()
 
 
+def _queries(cache: KVCache, q, pages, q_start, max_q, window):
+    """What the queries' arguments come to -> (B, max_pages, pointer of q_start, max_q, window)."""
+    B, max_pages = pages.shape
+    qs = 0
+    if max_q is None:
+        if q_start is not None:
+            raise ValueError("q_start needs max_q")
+        max_q = max(1, q.shape[0] // max(1, B))                       # (no sequence: the library refuses it)
+    if q_start is not None:
+        qs = _array(q_start, "q_start", cache, torch.int32, (B + 1,))
+    if max_q >> 31 or window >> 31:                                   # below 0, which the library refuses, or beyond it
+        window = min(window, 2 ** 31 - 1)                             # (no sequence is that long)
+        _int32(max_q=max_q, window=window)
+    return B, max_pages, qs, max_q, window
+
+
 def fk_kv_attend(cache: KVCache, q, pages, lens, *, q_start=None, max_q=None, max_len: int = 0, scale=None, causal: bool = True,
                  window: int = 0, lse: bool = False, ws=None, out=None):
     """q [Tq, q_heads, d] against the cached sequences: pages [B, max_pages] int32, lens [B] int32.  The queries of sequence b are
@@ -476,17 +504,7 @@ def fk_kv_attend(cache: KVCache, q, pages, lens, *, q_start=None, max_q=None, ma
     ref = cache._here()
     Tq, heads, _ = q.shape
     qp, qt, qh = _rows(q, "q", cache, Tq, heads)
-    B, max_pages = pages.shape
-    qs = 0
-    if max_q is None:
-        if q_start is not None:
-            raise ValueError("q_start needs max_q")
-        max_q = max(1, Tq // max(1, B))                               # (no sequence: the library refuses it)
-    if q_start is not None:
-        qs = _array(q_start, "q_start", cache, torch.int32, (B + 1,))
-    if max_q >> 31 or window >> 31:                                   # below 0, which the library refuses, or beyond it
-        window = min(window, 2 ** 31 - 1)                             # (no sequence is that long)
-        _int32(max_q=max_q, window=window)
+    B, max_pages, qs, max_q, window = _queries(cache, q, pages, q_start, max_q, window)
     if not max_len:
         max_len = max_pages * cache.page_size
     if ws is None:
@@ -499,3 +517,99 @@ def fk_kv_attend(cache: KVCache, q, pages, lens, *, q_start=None, max_q=None, ma
                               op, le.data_ptr() if lse else 0,
                               _array(ws, "ws", cache, torch.uint8, ws.shape), ws.numel(), _raw_stream(cache)))
     return (out, le) if lse else out
+
+
+def fk_kv_attend_tree(cache: KVCache, q, pages, lens, tree, *, q_start=None, max_q=None, max_len: int = 0, scale=None, window: int = 0,
+                      lse: bool = False, ws=None, out=None):
+    """fk_kv_attend for a tree of drafted tokens, the last ones of each sequence: query i sees what lies before the tree and the
+    tree's tokens j whose bit j % 64 of tree[i, j // 64] is set (tree [Tq, words] int64; kv_cache.tree_masks makes it)."""
+    ref = cache._here()
+    Tq, heads, _ = q.shape
+    qp, qt, qh = _rows(q, "q", cache, Tq, heads)
+    B, max_pages, qs, max_q, window = _queries(cache, q, pages, q_start, max_q, window)
+    if tree.dim() != 2:
+        raise ValueError("tree must be [Tq, words]")
+    words = tree.shape[1]
+    _int32(words=words)
+    if not max_len:
+        max_len = max_pages * cache.page_size
+    if ws is None:
+        ws = make_kv_workspace(cache, B, heads, Tq, max_q, max_len)
+    out, op = _result(out, "out", cache, q, (Tq, heads, cache.d))
+    le = torch.empty((Tq, heads), dtype=torch.float32, device=cache.device) if lse else None
+    _check(lib().fk_kv_attend_tree(ref, qp, qt, qh, heads, Tq, _array(pages, "pages", cache, torch.int32, (B, max_pages)), max_pages,
+                                   _array(lens, "lens", cache, torch.int32, (B,)), qs, B, max_q, max_len,
+                                   cache.d ** -0.5 if scale is None else scale, window,
+                                   _array(tree, "tree", cache, torch.int64, (Tq, words)), words, op, le.data_ptr() if lse else 0,
+                                   _array(ws, "ws", cache, torch.uint8, ws.shape), ws.numel(), _raw_stream(cache)))
+    return (out, le) if lse else out
+
+
+def fk_kv_weigh(cache: KVCache, q, lse, pages, lens, mass, *, q_start=None, max_q=None, max_len: int = 0, scale=None, causal: bool = True,
+                window: int = 0, known=None, decay: float = 1.0, out=None):
+    """The attention weights of q [Tq, q_heads, d], whose softmax sums have the logarithms lse [Tq, q_heads] float32 (fk_kv_attend gives
+    them), added up for every token and cache head into mass [pages, heads, page_size] float32, or into `out` beside it.  Tokens from
+    place known[b] on ([B] int32) have no weights yet; older ones fade by `decay`.  -> mass, or out"""
+    ref = cache._here()
+    Tq, heads, _ = q.shape
+    qp, qt, qh = _rows(q, "q", cache, Tq, heads)
+    B, max_pages, qs, max_q, window = _queries(cache, q, pages, q_start, max_q, window)
+    shape = (cache.pages, cache.heads, cache.page_size)
+    mp = _array(mass, "mass", cache, torch.float32, shape)
+    op = mp if out is None else _array(out, "out", cache, torch.float32, shape)
+    _check(lib().fk_kv_weigh(ref, qp, qt, qh, heads, Tq, _array(lse, "lse", cache, torch.float32, (Tq, heads)),
+                             _array(pages, "pages", cache, torch.int32, (B, max_pages)), max_pages,
+                             _array(lens, "lens", cache, torch.int32, (B,)), qs, B, max_q, max_len,
+                             cache.d ** -0.5 if scale is None else scale, causal, window,
+                             0 if known is None else _array(known, "known", cache, torch.int32, (B,)), decay, mp, op, _raw_stream(cache)))
+    return mass if out is None else out
+
+
+def fk_kv_choose(cache: KVCache, mass, pages, lens, keep: int, *, first: int = 0, last: int = 0, max_len: int = 0, kept=None, counts=None,
+                 ws=None):
+    """The places that stay when sequences are cut down to `keep` tokens: the first ones, the last ones, and those with the largest weights
+    mass [pages, heads, page_size] float32, for each head -> (kept [B, heads, keep] int32, ascending, -1 behind them; counts [B] int32)."""
+    ref = cache._here()
+    B, max_pages = pages.shape
+    _int32(keep=keep, first=first, last=last)
+    L = lib()
+    if kept is None:
+        kept = torch.empty((B, cache.heads, max(keep, 0)), dtype=torch.int32, device=cache.device)
+    if counts is None:
+        counts = torch.empty_like(lens)
+    if not max_len:
+        max_len = max_pages * cache.page_size
+    if ws is None:
+        n = L.fk_kv_choose_workspace_bytes(ref, B, max_len)
+        ws = torch.empty(n, dtype=torch.uint8, device=cache.device) if n else None
+    _check(L.fk_kv_choose(ref, _array(mass, "mass", cache, torch.float32, (cache.pages, cache.heads, cache.page_size)),
+                          _array(pages, "pages", cache, torch.int32, (B, max_pages)), max_pages,
+                          _array(lens, "lens", cache, torch.int32, (B,)), B, max_len, keep, first, last,
+                          _array(kept, "kept", cache, torch.int32, (B, cache.heads, keep)),
+                          _array(counts, "counts", cache, torch.int32, (B,)),
+                          0 if ws is None else _array(ws, "ws", cache, torch.uint8, ws.shape), 0 if ws is None else ws.numel(),
+                          _raw_stream(cache)))
+    return kept, counts
+
+
+def fk_kv_compact(cache: KVCache, pages, kept, counts, *, start=None, to_pages=None, mass=None):
+    """Moves rows to the front of their sequences: place start[b] + j gets the row of place start[b] + kept[b, h, j], for j < counts[b]
+    (kept [B, heads or 1, most] int32, ascending; counts, start [B] int32), and mass [pages, heads, page_size] float32 likewise; in place, or
+    into the pages of to_pages [B, max_pages] int32."""
+    ref = cache._here()
+    B, max_pages = pages.shape
+    if kept.dim() != 3:
+        raise ValueError("kept must be [B, heads or 1, places]")
+    _, heads, most = kept.shape
+    to, to_max = 0, 0
+    if to_pages is not None:
+        if to_pages.dim() != 2:
+            raise ValueError("to_pages must be [B, max_pages]")
+        to_max = to_pages.shape[1]
+        to = _array(to_pages, "to_pages", cache, torch.int32, (B, to_max))
+    _check(lib().fk_kv_compact(ref, _array(pages, "pages", cache, torch.int32, (B, max_pages)), max_pages,
+                               _array(kept, "kept", cache, torch.int32, (B, heads, most)), heads, most,
+                               _array(counts, "counts", cache, torch.int32, (B,)),
+                               0 if start is None else _array(start, "start", cache, torch.int32, (B,)), to, to_max, B,
+                               0 if mass is None else _array(mass, "mass", cache, torch.float32,
+                                                             (cache.pages, cache.heads, cache.page_size)), _raw_stream(cache)))

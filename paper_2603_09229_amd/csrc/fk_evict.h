@@ -1,0 +1,50 @@
+// Internal declarations of what keeps a 4-bit key/value cache small: attention weights, choice of places, compaction (not part of the ABI).
+#pragma once
+
+#include "fk_kv.h"
+
+namespace fk {
+
+struct KVWeigh {
+    KVRows q;
+    int q_heads;
+    int64_t Tq;
+    const float* lse;
+    const int32_t *pages, *lens, *q_start;
+    int max_pages, B, max_q;
+    float scale;
+    int causal, window;
+    const int32_t* known;
+    float decay;
+    const float* mass;
+    float* out;
+};
+
+struct KVChoose {
+    const float* mass;
+    const int32_t *pages, *lens;
+    int max_pages, B, keep, first, last;
+    int32_t *kept, *counts;
+};
+
+struct KVCompact {
+    const int32_t *pages, *to_pages;
+    int max_pages, to_max_pages, B;
+    const int32_t *kept, *counts, *start;
+    int max_kept, kept_heads;
+    float* mass;
+};
+
+// How a call that weighs is divided.
+struct KVWeighPlan {
+    int row_waves;        // waves of a workgroup that share its tokens and divide the query rows
+    int64_t chunk;        // tokens of a workgroup
+    int blocks;           // workgroups along the tokens
+};
+KVWeighPlan choose_weigh_plan(const KVView& c, int q_heads, int B, int max_q, int64_t max_len);
+
+fk_status launch_kv_weigh(const KVView& c, const KVWeigh& a, const KVWeighPlan& p, hipStream_t s);
+fk_status launch_kv_choose(const KVView& c, const KVChoose& a, int64_t max_len, hipStream_t s);
+fk_status launch_kv_compact(const KVView& c, const KVCompact& a, hipStream_t s);
+
+}  // namespace fk

@@ -58,6 +58,8 @@ struct KVAttend {
     uint16_t* out;
     float* lse;
     float* part;          // workspace: see kv_partial_floats
+    const uint64_t* tree = nullptr;   // a tree's mask: `words` of each query token
+    int words = 0;
 };
 
 // Waves of a workgroup with rows of their own: four, two workgroups to a compute unit; with one tile each eight, that share one table.
@@ -78,6 +80,15 @@ inline int64_t kv_partial_floats(const KVPlan& p, int d) { return (int64_t)p.til
 inline size_t kv_partial_bytes(const KVPlan& p, int d, int heads, int B) {
     return p.splits <= 1 ? 0 : (size_t)B * heads * p.row_blocks * p.splits * kv_partial_floats(p, d) * 4;
 }
+
+// Checks of arguments (fk_kv_api.hip).
+// The cache as the kernels see it, of which the tensors are looked at only with `pointers`; false sets the error and why.
+bool view_of(const char* fn, const fk_kv_cache* c, bool pointers, KVView* v, fk_status* why);
+// A device pointer that has to be there, aligned to `to` bytes.
+fk_status need(const char* fn, const char* name, const void* p, size_t to);
+fk_status check_queries(const char* fn, const KVView& c, int q_heads, int64_t Tq, int B, int max_q, int64_t max_len);
+// The most tokens that the queries of a sequence see together.
+int64_t reach_of(int window, int max_q, int64_t max_len);
 
 fk_status launch_kv_append(const KVView& c, const KVAppend& a, hipStream_t s);
 fk_status launch_kv_read(const KVView& c, const int64_t* slots, int64_t T, uint16_t* k_out, uint16_t* v_out, hipStream_t s);

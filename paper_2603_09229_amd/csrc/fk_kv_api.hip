@@ -8,7 +8,7 @@
 
 namespace fk {
 
-static bool view_of(const char* fn, const fk_kv_cache* c, bool pointers, KVView* v, fk_status* why) {
+bool view_of(const char* fn, const fk_kv_cache* c, bool pointers, KVView* v, fk_status* why) {
     *why = FK_EINVAL;
     if (!c) {
         set_error("%s: the cache is NULL", fn);
@@ -46,14 +46,13 @@ static bool view_of(const char* fn, const fk_kv_cache* c, bool pointers, KVView*
     return true;
 }
 
-// A device pointer that has to be there, aligned to `to` bytes.
-static fk_status need(const char* fn, const char* name, const void* p, size_t to) {
+fk_status need(const char* fn, const char* name, const void* p, size_t to) {
     if (p && !((uintptr_t)p & (to - 1))) return FK_OK;
     set_error("%s: %s is NULL or not %zu-byte aligned", fn, name, to);
     return FK_EINVAL;
 }
 
-static fk_status check_queries(const char* fn, const KVView& c, int q_heads, int64_t Tq, int B, int max_q, int64_t max_len) {
+fk_status check_queries(const char* fn, const KVView& c, int q_heads, int64_t Tq, int B, int max_q, int64_t max_len) {
     if (q_heads < 1 || B < 1 || max_q < 1 || Tq < 0 || max_len < 0) {
         set_error("%s: q_heads, B, max_q must be positive, Tq and max_len not negative (%d, %d, %d, %lld, %lld)", fn, q_heads, B,
                   max_q, (long long)Tq, (long long)max_len);
@@ -70,8 +69,7 @@ static fk_status check_queries(const char* fn, const KVView& c, int q_heads, int
     return FK_OK;
 }
 
-// The most tokens that the queries of a sequence see together.
-static int64_t reach_of(int window, int max_q, int64_t max_len) {
+int64_t reach_of(int window, int max_q, int64_t max_len) {
     return window ? std::min((int64_t)window + max_q - 1, max_len) : max_len;
 }
 

@@ -1,4 +1,5 @@
-// Attention over the 4-bit key/value cache.
+// Attention over the 4-bit key/value cache: kernels and their launches, for queries in a row (fk_kv_attend.hip) and for trees of drafted
+// tokens (fk_tree_attend.hip).
 //
 // For query row n and tokens j: x_j = scale s_j (q_n . K_j), out = sum_j 2^(x_j log2 e - m) s'_j V_j / sum_j 2^(x_j log2 e - m),
 // K_j and V_j rows of levels, s_j and s'_j the rows' scales.  A wave keeps 16 * NT query rows (a row: one head of the
@@ -33,6 +34,8 @@
 // Many rows: vector instructions.  A step of 48 rows and 32 tokens at d = 128 takes 48 MFMA (768 cycles), 64 lookups and about 240 vector
 // instructions with 24 exponentials (1340 cycles); two waves a SIMD overlap a third of the two.  Two sequences of 4096 queries over up to
 // 9000 tokens, 32 query heads: 852 GFLOP in 1058 us, 0.8 PFLOP/s (the first 30 passes of a program 1130); a large product of the library reaches 1.2 on this card.
+#pragma once
+
 #include <algorithm>
 
 #include "fk_device.h"
@@ -279,17 +282,59 @@ struct Place {
     }
 };
 
-// The tokens that a wave's rows see: all of [lo, hi) is seen by some row; the row of column c, at position pos[c], sees those of
+// The tokens that a wave's rows see: all of [lo, hi) may be seen by some row; the row of column c, at position pos[c], sees those of
 // [0, hi) that are more than `before` and at most `after` from it.
-template <int NT>
+template <int NT, bool TREE>
 struct Seen {
     int lo, hi, before, after, pos[NT];
 };
+// Trees: it sees those from `from` on that lie before `base` or whose bit is set in the 32-bit words at byte `row` of the mask.
+template <int NT>
+struct Seen<NT, true> {
+    int lo, hi, base, words, from[NT];
+    uint32_t row[NT];
+    Base mask;
+
+    // bits of the 32 tokens from `token` on for column c: all set before the tree, none behind the mask
+    __device__ __forceinline__ uint32_t bits(int c, int token) const {
+        const int j = token - base, w = j >> 5;
+        uint32_t two[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            two[i] = w + i < 0 ? ~0u : 0u;
+            if (w + i >= 0 && w + i < words) two[i] = load_at<uint32_t>(mask, row[c] + 4 * (w + i));
+        }
+        return __builtin_amdgcn_alignbit(two[1], two[0], j & 31);
+    }
+};
+
+// The first token that a row of a tree sees: of those before the tree and the marked ones of its n, in order, the last `window`.
+__device__ __forceinline__ int tree_from(const uint64_t* row, int words, int base, int n, int window) {
+    auto word = [&](int w) {                                      // without the bits behind the tree and before the sequence
+        uint64_t x = row[w];
+        const int over = n - 64 * w, under = -base - 64 * w;
+        if (over < 64) x &= ((uint64_t)1 << over) - 1;
+        if (under > 0) x = under < 64 ? x >> under << under : 0;
+        return x;
+    };
+    const int all = min(words, (n + 63) / 64);
+    int left = window;
+    for (int w = all - 1; w >= 0; --w) {
+        uint64_t x = word(w);
+        int has = __popcll(x);
+        if (has >= left) {
+            for (; has > left; --has) x &= x - 1;
+            return base + 64 * w + __ffsll((unsigned long long)x) - 1;
+        }
+        left -= has;
+    }
+    return base - left;
+}
 
 // Query rows from row0 on: the operand, and where the columns' rows are.
-template <int ND, int NT>
+template <int ND, int NT, bool TREE>
 __device__ __forceinline__ void load_queries(const AttendArgs& A, const Place& p, int h, int row0, int n, int q, uintx4 (&Q)[NT][ND],
-                                             Seen<NT>& seen) {
+                                             Seen<NT, TREE>& seen) {
     const KVAttend& a = A.a;
 #pragma unroll
     for (int c = 0; c < NT; ++c) {
@@ -301,10 +346,22 @@ __device__ __forceinline__ void load_queries(const AttendArgs& A, const Place& p
             Q[c][k] = uintx4{0, 0, 0, 0};
             if (live) Q[c][k] = *(const uintx4_any*)(at + 8 * k) ^ A.flip;
         }
-        seen.pos[c] = p.len - p.nq + i;
+        if constexpr (TREE) {
+            const int64_t at = p.q0 + (live ? i : 0);             // (a wave without rows asks for no bits)
+            seen.row[c] = (uint32_t)(at * a.words * 8);
+            seen.from[c] = a.window && live ? tree_from(a.tree + at * a.words, a.words, p.len - p.nq, p.nq, a.window) : 0;
+        } else {
+            seen.pos[c] = p.len - p.nq + i;
+        }
     }
-    seen.after = a.causal ? 0 : INT32_MAX;
-    seen.before = a.window ? -a.window : INT32_MIN;
+    if constexpr (TREE) {
+        seen.base = p.len - p.nq;
+        seen.words = 2 * a.words;
+        seen.mask = base_of(a.tree, 0);
+    } else {
+        seen.after = a.causal ? 0 : INT32_MAX;
+        seen.before = a.window ? -a.window : INT32_MIN;
+    }
 }
 
 // 1 / sum, 0 for a row that has seen nothing; and its lse (top in powers of two)
@@ -331,9 +388,9 @@ struct Softmax {
     // reference.  The lane's e-th score is of token first + 16 (e / 4) + e % 4, vs has its values' scales, 16 bits
     // each, and loses those that must not be multiplied.  A column's reference depends on what its row sees and on nothing else: other columns'
     // scores and scales that the row does not see may bring the wave to the branch, but do not move it there.
-    template <bool BF>
+    template <bool BF, bool TREE>
     __device__ __forceinline__ void step(const floatx4 (&X)[2][NT], const float (&ks)[8], uintx2 (&vs)[2], bool masked,
-                                         const Seen<NT>& seen, int first, floatx4 (&O)[S][NT], uintx4 (&w)[NT]) {
+                                         const Seen<NT, TREE>& seen, int first, floatx4 (&O)[S][NT], uintx4 (&w)[NT]) {
         float x[NT][8], peak[NT];
 #pragma unroll
         for (int c = 0; c < NT; ++c)
@@ -346,12 +403,20 @@ struct Softmax {
         };
         uint16_t most = largest();
         if (masked) {
+            uint32_t open[NT];
+            if constexpr (TREE) {
+                const int quarter = (threadIdx.x >> 2) & 12;      // 4q, of the step's 32 tokens
+#pragma unroll
+                for (int c = 0; c < NT; ++c) open[c] = seen.bits(c, __builtin_amdgcn_readfirstlane(first - quarter)) >> quarter;
+            }
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const int token = first + 16 * (e / 4) + (e & 3);
 #pragma unroll
                 for (int c = 0; c < NT; ++c)
-                    x[c][e] = token >= seen.hi || token - seen.pos[c] > seen.after || token - seen.pos[c] <= seen.before ? -INFINITY : x[c][e];
+                    if constexpr (TREE)
+                        x[c][e] = token >= seen.hi || token < seen.from[c] || !(open[c] >> (16 * (e / 4) + (e & 3)) & 1) ? -INFINITY : x[c][e];
+                    else x[c][e] = token >= seen.hi || token - seen.pos[c] > seen.after || token - seen.pos[c] <= seen.before ? -INFINITY : x[c][e];
             }
             // A value's scale that is not finite goes straight to the sums of the rows that see it, and is not multiplied where none does; past the
             // end it may be anything, signs included.
@@ -447,7 +512,7 @@ struct Softmax {
 // JOIN: the waves of a workgroup share the rows and divide the tokens, each takes every kJoinWaves-th step (and workgroups may divide them
 // further); otherwise each wave has rows of its own, of one sequence or, where that has fewer tiles than a workgroup has waves, of
 // several, and takes all steps that they see.  Codes go straight from the cache into operands.
-template <bool BF, int ND, int NT, bool JOIN>
+template <bool BF, int ND, int NT, bool JOIN, bool TREE>
 __global__ __launch_bounds__(64 * (JOIN ? kJoinWaves : own_waves(NT)), NT == 1 && ND <= 4 ? 4 : JOIN ? 1 : 2)
 void kv_attend_kernel(AttendArgs A) {
     // (a fixed size, so that the compiler knows the table's address and leaves it to the instruction's offset)
@@ -497,23 +562,24 @@ void kv_attend_kernel(AttendArgs A) {
 
     // tokens that the wave's rows see
     const int i0 = A.group.quotient(row0), i1 = A.group.quotient(max(min(row0 + R, rows) - 1, 0));
-    const int p0 = len - nq + i0, p1 = len - nq + i1;
+    // (in a tree a row may see no token but those before it, or all)
+    const int p0 = len - nq + (TREE ? -1 : i0), p1 = len - nq + (TREE ? nq : i1 + 1) - 1;
     const int hi = row0 >= rows ? 0 : a.causal ? max(min(len, p1 + 1), 0) : len;
     const int lo = a.window ? max(0, p0 - a.window + 1) : 0;
     const int first = (lo & ~(kStep - 1)) + (JOIN ? split * A.chunk : 0);
     const int end = !JOIN || split == A.splits - 1 ? hi : min(hi, first + A.chunk);
     if (JOIN && split > 0 && first >= hi) return;                 // the whole workgroup
     // a step is whole where every row sees all of its tokens
-    const int whole_end = a.causal ? min(len, p0 + 1) : len, whole_from = a.window ? p1 - a.window + 1 : 0;
+    const int whole_end = TREE || a.causal ? min(len, p0 + 1) : len, whole_from = a.window ? p1 - a.window + 1 : 0;
     mine = first + (JOIN ? wave * kStep : 0);
     const int steps = end > mine ? (end - mine + W * kStep - 1) / (W * kStep) : 0;
     if (a.window && steps) begin();
 
     uintx4 Q[NT][ND];
-    Seen<NT> seen;
+    Seen<NT, TREE> seen;
     seen.lo = lo;
     seen.hi = hi;
-    load_queries<ND, NT>(A, at, h, row0, n, q, Q, seen);
+    load_queries<ND, NT, TREE>(A, at, h, row0, n, q, Q, seen);
     const float down = T::fill<BF, THREADS>(lds, level, lane);
 
     floatx4 O[S][NT];
@@ -557,7 +623,7 @@ void kv_attend_kernel(AttendArgs A) {
         in.load_scales(f, row);
         if constexpr (!JOIN) __builtin_amdgcn_sched_barrier(0);
         uintx4 w[NT];
-        soft.template step<BF>(X, ks, vs, from + kStep > whole_end || from < whole_from,   // some row does not see all of these tokens
+        soft.template step<BF, TREE>(X, ks, vs, from + kStep > whole_end || from < whole_from,   // some row does not see all of these tokens
                                seen, from + 4 * q, O, w);
 
         if constexpr (!JOIN) __builtin_amdgcn_sched_barrier(0);
@@ -724,7 +790,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void kv_join_kernel(AttendArgs A) {
     if (row0 + c * 16 >= rows) return;
     const int i0 = A.group.quotient(row0), i1 = A.group.quotient(min(row0 + R, rows) - 1);
     const int hi = a.causal ? max(min(len, len - nq + i1 + 1), 0) : len;
-    const int lo = (a.window ? max(0, len - nq + i0 - a.window + 1) : 0) & ~(kStep - 1);
+    const int lo = (a.window ? max(0, len - nq + (a.tree ? -1 : i0) - a.window + 1) : 0) & ~(kStep - 1);
     if (hi - lo <= A.chunk) return;                               // one split has written the result itself
     const int parts = min(A.splits, (hi - lo + A.chunk - 1) / A.chunk);
 
@@ -783,58 +849,9 @@ __global__ __launch_bounds__(64 * WAVES, 4) void kv_join_kernel(AttendArgs A) {
 static constexpr int own_tiles(int ND) { return ND <= 2 ? 4 : ND <= 4 ? 3 : ND <= 6 ? 2 : 1; }
 static constexpr int join_tiles(int ND) { return ND <= 2 ? 4 : ND <= 4 ? 3 : ND <= 6 ? 2 : 1; }
 
-KVPlan choose_kv_plan(const KVView& c, int q_heads, int B, int max_q, int64_t reach) {
-    const int group = q_heads / c.heads, ND = c.d / 32;
-    const int64_t rows = (int64_t)max_q * group, units = device_cu_count();
-    KVPlan p;
-    p.splits = 1;
-    p.chunk = INT32_MAX / 2;
-    // Waves with rows of their own need no exchange at the end, but the rows' workgroups alone have to fill the chip (8 x 5 queries of 16
-    // heads of 256 over 4000 tokens: 16 workgroups 235 us, divided by tokens too 23); otherwise the tokens are divided.
-    const int64_t own_blocks = (int64_t)B * c.heads * cdiv(rows, 16 * own_tiles(ND) * own_waves(own_tiles(ND)));
-    if (rows > 16 * join_tiles(ND) && own_blocks >= units) {
-        p.join = false;
-        p.tiles = own_tiles(ND);
-        p.row_blocks = (int)cdiv(rows, 16 * p.tiles);
-        return p;
-    }
-    p.join = true;
-    p.tiles = (int)std::min(cdiv(rows, 16), (int64_t)join_tiles(ND));
-    p.row_blocks = (int)cdiv(rows, 16 * p.tiles);
-    // One workgroup to a compute unit: 8 heads, one sequence of 131072 tokens 64 splits 38.2 us, 32 35.6, 24 41.4.
-    const int64_t wg = kJoinWaves * kStep, blocks = (int64_t)B * c.heads * p.row_blocks;
-    const int64_t want = blocks >= units ? 1 : units / blocks, steps = cdiv(reach, wg);
-    // Splitting costs the second launch, about four steps of a workgroup: 8 heads of 128, one sequence of 700 tokens (3 steps) 10.1 us
-    // in one piece and 10.0 in three, of 1500 (6) 13.8 and 10.4 in six; 24 sequences of 2048 (8), 4 heads of 64, 13.3 and 13.0 in two.
-    p.splits = (int)std::min({want, steps, (int64_t)kMostSplits});
-    if (steps - cdiv(steps, p.splits) <= 4) p.splits = 1;
-    if (p.splits > 1) {
-        p.chunk = cdiv(steps, p.splits) * wg;
-        return p;
-    }
-    // Many short sequences: a tile to a wave, eight to a workgroup, saves the workgroups' fixed cost and gives up dividing the tokens.  In tenths of a
-    // microsecond, fitted to 986 measured pairs from 32 to 256 channels, 1 to 4 tiles and 9 to 500 tokens (of which it takes the slower one where that
-    // costs 0.6 % on average, and tiles where they are up to 2 % slower): workgroups that share their rows and hold at most 128 registers run in
-    // pairs on a compute unit, others in rounds; each takes a time of its own and one a step of 256 tokens.  Tiles take theirs a step of 32.
-    // One query of 4 heads to each of 8 heads of 128: 64 sequences of 100 tokens 10.3 us shared and 10.7 in tiles, of 32 9.5 and 6.6; 128 of 300
-    // 23 and 18; of 256 channels 64 of 200 22.6 and 21.5, 32 of 200 12.4 and 21.2.
-    const int64_t tiles = cdiv(rows, 16), own = cdiv(B * tiles, 8) * c.heads, more = std::max(blocks - units, (int64_t)0),
-                  more_own = std::max(own - units, (int64_t)0), w = ND * p.tiles, own_steps = cdiv(reach, kStep);
-    const bool pairs = w <= 2 || (p.tiles == 1 && ND <= 4);
-    const int64_t shared_cost = pairs ? (40 + 5 * w + (4 + 3 * w) * steps) * units + (15 + w + (7 + 2 * w) * steps) * more
-                                      : (60 + 2 * w + (10 + 2 * w) * steps) * cdiv(blocks, units) * units;
-    const int64_t own_cost = (38 + 4 * ND + (7 + 2 * ND) * own_steps) * units + (15 + 9 * ND + (6 + 6 * ND) * own_steps) * more_own;
-    if (own_cost < shared_cost) {
-        p.join = false;
-        p.tiles = 1;
-        p.row_blocks = (int)tiles;
-    }
-    return p;
-}
-
-template <bool BF, int ND, int NT>
+template <bool BF, int ND, int NT, bool TREE>
 static fk_status launch_form(const AttendArgs& A, hipStream_t s) {
-    kv_attend_kernel<BF, ND, NT, true><<<dim3(A.row_blocks * A.splits, A.c.heads, A.a.B), 64 * kJoinWaves, 0, s>>>(A);
+    kv_attend_kernel<BF, ND, NT, true, TREE><<<dim3(A.row_blocks * A.splits, A.c.heads, A.a.B), 64 * kJoinWaves, 0, s>>>(A);
     FK_HIP(hipGetLastError());
     if (A.splits > 1) {
         const dim3 grid(A.row_blocks * 2 * ND * NT, A.c.heads, A.a.B);
@@ -845,46 +862,47 @@ static fk_status launch_form(const AttendArgs& A, hipStream_t s) {
     return FK_OK;
 }
 
-template <bool BF, int ND>
+template <bool BF, int ND, bool TREE>
 static fk_status launch_width(const AttendArgs& A, const KVPlan& p, hipStream_t s) {
     if (!p.join) {
         const int waves = own_waves(p.tiles);
         const int64_t blocks = (A.row_blocks < waves ? cdiv((int64_t)A.a.B * A.row_blocks, waves) : cdiv(A.row_blocks, waves) * A.a.B) * A.c.heads;
         if (blocks > INT32_MAX / 512) {
-            set_error("fk_kv_attend: unsupported size: %lld workgroups", (long long)blocks);
+            set_error("%s: unsupported size: %lld workgroups", TREE ? "fk_kv_attend_tree" : "fk_kv_attend", (long long)blocks);
             return FK_EUNSUPPORTED;
         }
-        if (p.tiles == 1) kv_attend_kernel<BF, ND, 1, false><<<(unsigned)blocks, 64 * own_waves(1), 0, s>>>(A);
+        if (p.tiles == 1) kv_attend_kernel<BF, ND, 1, false, TREE><<<(unsigned)blocks, 64 * own_waves(1), 0, s>>>(A);
         else if constexpr (own_tiles(ND) > 1)
-            kv_attend_kernel<BF, ND, own_tiles(ND), false><<<(unsigned)blocks, 64 * own_waves(own_tiles(ND)), 0, s>>>(A);
+            kv_attend_kernel<BF, ND, own_tiles(ND), false, TREE><<<(unsigned)blocks, 64 * own_waves(own_tiles(ND)), 0, s>>>(A);
         FK_HIP(hipGetLastError());
         return FK_OK;
     }
-    if (p.tiles == 1) return launch_form<BF, ND, 1>(A, s);
+    if (p.tiles == 1) return launch_form<BF, ND, 1, TREE>(A, s);
     if constexpr (join_tiles(ND) >= 2)
-        if (p.tiles == 2) return launch_form<BF, ND, 2>(A, s);
+        if (p.tiles == 2) return launch_form<BF, ND, 2, TREE>(A, s);
     if constexpr (join_tiles(ND) >= 3)
-        if (p.tiles == 3) return launch_form<BF, ND, 3>(A, s);
-    return launch_form<BF, ND, join_tiles(ND)>(A, s);
+        if (p.tiles == 3) return launch_form<BF, ND, 3, TREE>(A, s);
+    return launch_form<BF, ND, join_tiles(ND), TREE>(A, s);
 }
 
-template <bool BF>
+template <bool BF, bool TREE>
 static fk_status launch_type(const AttendArgs& A, const KVPlan& p, hipStream_t s) {
     switch (A.c.d / 32) {
-        case 1: return launch_width<BF, 1>(A, p, s);
-        case 2: return launch_width<BF, 2>(A, p, s);
-        case 3: return launch_width<BF, 3>(A, p, s);
-        case 4: return launch_width<BF, 4>(A, p, s);
-        case 5: return launch_width<BF, 5>(A, p, s);
-        case 6: return launch_width<BF, 6>(A, p, s);
-        case 7: return launch_width<BF, 7>(A, p, s);
-        default: return launch_width<BF, 8>(A, p, s);
+        case 1: return launch_width<BF, 1, TREE>(A, p, s);
+        case 2: return launch_width<BF, 2, TREE>(A, p, s);
+        case 3: return launch_width<BF, 3, TREE>(A, p, s);
+        case 4: return launch_width<BF, 4, TREE>(A, p, s);
+        case 5: return launch_width<BF, 5, TREE>(A, p, s);
+        case 6: return launch_width<BF, 6, TREE>(A, p, s);
+        case 7: return launch_width<BF, 7, TREE>(A, p, s);
+        default: return launch_width<BF, 8, TREE>(A, p, s);
     }
 }
 
-fk_status launch_kv_attend(const KVView& c, const KVAttend& a, const KVPlan& p, hipStream_t s) {
+template <bool TREE>
+static fk_status launch_attend(const KVView& c, const KVAttend& a, const KVPlan& p, hipStream_t s) {
     const AttendArgs A{c, a, Divider(a.q_heads / c.heads), p.splits, p.row_blocks, (int)p.chunk, fmaxf(fabsf(a.scale) * 1.44269504088896341f, 1e-37f), a.scale < 0.f ? 0x80008000u : 0u};
-    return c.bf ? launch_type<true>(A, p, s) : launch_type<false>(A, p, s);
+    return c.bf ? launch_type<true, TREE>(A, p, s) : launch_type<false, TREE>(A, p, s);
 }
 
 }  // namespace fk

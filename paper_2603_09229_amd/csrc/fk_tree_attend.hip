@@ -1,0 +1,58 @@
+// Attention of a tree of drafted tokens over the 4-bit key/value cache: the kernels of fk_kv_attend.h, with the tree's mask.
+//
+// The n queries of a sequence are its last n tokens, which are in the cache already.  All of them see what lies before the tree, which is
+// where nearly all of the time goes and where nothing differs from queries in a row; of the tree's own n tokens they see those whose bits are set.  So the
+// mask is only looked at in the steps of 32 tokens that reach past the prefix, two words a row and step, shifted to the step's first
+// token; the bits of tokens before the tree count as set, so that a step may begin anywhere.
+#include "fk_kv_attend.h"
+
+using namespace fk;
+
+extern "C" fk_status fk_kv_attend_tree(const fk_kv_cache* cache, const void* q, int64_t q_token_stride, int64_t q_head_stride, int q_heads,
+                                       int64_t Tq, const int32_t* pages, int max_pages, const int32_t* lens, const int32_t* q_start, int B,
+                                       int max_q, int64_t max_len, float scale, int window, const uint64_t* tree, int words, void* out,
+                                       float* lse, void* ws, size_t ws_bytes, void* stream) {
+    const char* fn = "fk_kv_attend_tree";
+    KVView c;
+    fk_status why;
+    if (!view_of(fn, cache, true, &c, &why)) return why;
+    FK_TRY(check_queries(fn, c, q_heads, Tq, B, max_q, max_len));
+    if (max_pages < 1 || window < 0 || (!q_start && Tq != (int64_t)B * max_q)) {
+        set_error("%s: max_pages=%d, window=%d, or Tq=%lld without q_start is not B * max_q", fn, max_pages, window, (long long)Tq);
+        return FK_EINVAL;
+    }
+    if (words < 1 || (int64_t)words * 64 < max_q) {
+        set_error("%s: %d words of 64 bits for trees of up to %d tokens", fn, words, max_q);
+        return FK_EINVAL;
+    }
+    if (!(fabsf(scale) <= 1e38f)) {                               // (times log2 e it has to be finite)
+        set_error("%s: scale=%g is not a number up to 1e38", fn, (double)scale);
+        return FK_EINVAL;
+    }
+    // (a row of the mask is found by 32 bits)
+    if ((int64_t)max_pages << c.page_shift > (1 << 30) || Tq > (((int64_t)1 << 32) - 1) / 8 / words) {
+        set_error("%s: unsupported size max_pages=%d of %d tokens, or a mask of %lld x %d words", fn, max_pages, 1 << c.page_shift,
+                  (long long)Tq, words);
+        return FK_EUNSUPPORTED;
+    }
+    if (max_len == 0) max_len = (int64_t)max_pages << c.page_shift;
+    window = std::min(window, 1 << 30);
+    if (Tq == 0) return FK_OK;
+    FK_TRY(need(fn, "q", q, 2));
+    FK_TRY(need(fn, "pages", pages, 4));
+    FK_TRY(need(fn, "lens", lens, 4));
+    if (q_start) FK_TRY(need(fn, "q_start", q_start, 4));
+    FK_TRY(need(fn, "tree", tree, 8));
+    FK_TRY(need(fn, "out", out, 16));
+    if (lse) FK_TRY(need(fn, "lse", lse, 4));
+    FK_TRY(need(fn, "ws", ws, 256));
+    const KVPlan p = choose_kv_plan(c, q_heads, B, max_q, reach_of(window, max_q + 1, max_len));
+    const size_t bytes = kv_partial_bytes(p, c.d, c.heads, B);
+    if (ws_bytes < bytes) {
+        set_error("%s: workspace too small: %zu bytes given, %zu needed", fn, ws_bytes, bytes);
+        return FK_EWORKSPACE;
+    }
+    const KVAttend a{{(const uint16_t*)q, q_token_stride, q_head_stride}, q_heads, Tq, pages, lens, q_start, max_pages, B, max_q,
+                     scale, 0, window, (uint16_t*)out, lse, (float*)ws, tree, words};
+    return launch_attend<true>(c, a, p, (hipStream_t)stream);
+}
