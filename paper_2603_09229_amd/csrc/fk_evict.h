@@ -44,7 +44,8 @@ struct KVWeighPlan {
 KVWeighPlan choose_weigh_plan(const KVView& c, int q_heads, int B, int max_q, int64_t max_len);
 
 fk_status launch_kv_weigh(const KVView& c, const KVWeigh& a, const KVWeighPlan& p, hipStream_t s);
-fk_status launch_kv_choose(const KVView& c, const KVChoose& a, int64_t max_len, hipStream_t s);
+size_t choose_workspace_bytes(const KVView& c, int B, int64_t max_len);
+fk_status launch_kv_choose(const KVView& c, const KVChoose& a, int64_t max_len, void* ws, hipStream_t s);
 fk_status launch_kv_compact(const KVView& c, const KVCompact& a, hipStream_t s);
 
 }  // namespace fk

@@ -79,12 +79,27 @@ fk_status fk_kv_choose(const fk_kv_cache* cache, const float* mass, const int32_
     FK_TRY(need(fn, "lens", lens, 4));
     FK_TRY(need(fn, "kept", kept, 4));
     FK_TRY(need(fn, "counts", counts, 4));
+    max_len = max_len ? std::min(max_len, room) : room;
+    const size_t bytes = choose_workspace_bytes(c, B, max_len);
+    if (bytes) FK_TRY(need(fn, "ws", ws, 256));
+    if (ws_bytes < bytes) {
+        set_error("%s: workspace too small: %zu bytes given, %zu needed", fn, ws_bytes, bytes);
+        return FK_EWORKSPACE;
+    }
     const KVChoose a{mass, pages, lens, max_pages, B, keep, first, last, kept, counts};
-    return launch_kv_choose(c, a, max_len ? std::min(max_len, room) : room, (hipStream_t)stream);
+    return launch_kv_choose(c, a, max_len, ws, (hipStream_t)stream);
 }
 
 size_t fk_kv_choose_workspace_bytes(const fk_kv_cache* cache, int B, int64_t max_len) {
-    return 0;
+    const char* fn = "fk_kv_choose_workspace_bytes";
+    KVView c;
+    fk_status why;
+    if (!view_of(fn, cache, false, &c, &why)) return 0;
+    if (B < 1 || B > 65535 || max_len < 1 || max_len > (1 << 30)) {
+        set_error("%s: B=%d is not in 1..65535 or max_len=%lld not in 1..2^30", fn, B, (long long)max_len);
+        return 0;
+    }
+    return choose_workspace_bytes(c, B, max_len);
 }
 
 fk_status fk_kv_compact(const fk_kv_cache* cache, const int32_t* pages, int max_pages, const int32_t* kept, int kept_heads, int max_kept,
