@@ -37,6 +37,7 @@ struct KVCompact {
 
 // How a call that weighs is divided.
 struct KVWeighPlan {
+    bool stream;          // more query rows than a workgroup keeps
     int row_waves;        // waves of a workgroup that share its tokens and divide the query rows
     int64_t chunk;        // tokens of a workgroup
     int blocks;           // workgroups along the tokens
