@@ -405,7 +405,12 @@ fk_status fk_kv_attend_tree(const fk_kv_cache* cache, const void* q, int64_t q_t
 fk_status fk_kv_weigh(const fk_kv_cache* cache, const void* q, int64_t q_token_stride, int64_t q_head_stride, int q_heads,
                       int64_t Tq, const float* lse, const int32_t* pages, int max_pages, const int32_t* lens,
                       const int32_t* q_start, int B, int max_q, int64_t max_len, float scale, int causal, int window,
-                      const int32_t* known, float decay, const float* mass, float* mass_out, void* stream);
+                      const int32_t* known, float decay, const float* mass, float* mass_out, void* ws, size_t ws_bytes,
+                      void* stream);
+/* Device bytes that fk_kv_weigh needs in ws (256-byte aligned, contents undefined before and after); 0: none, and ws may be NULL (or
+ * unsupported, and fk_last_error says why).  Of the cache only the sizes and t are read; max_len >= 1, at most max_pages * page_size counts.  It
+ * holds for these sizes alone. */
+size_t fk_kv_weigh_workspace_bytes(const fk_kv_cache* cache, int q_heads, int64_t Tq, int B, int max_q, int64_t max_len);
 
 /*
  * The places that stay when a sequence of more than `keep` tokens is cut down to `keep`: its first `first` ones, its last `last` ones, and of the
@@ -416,6 +421,7 @@ fk_status fk_kv_weigh(const fk_kv_cache* cache, const void* q, int64_t q_token_s
  *   kept     device out, [B, heads, keep] int32: the places in ascending order, -1 behind them; all of a sequence of up to `keep` tokens
  *   counts   device out, [B] int32: min(lens, keep)
  *   ws       device, fk_kv_choose_workspace_bytes(...) bytes, 256-byte aligned, contents undefined before and after; NULL if that is 0
+ *            (max_len >= 1, at most max_pages * page_size counts)
  */
 fk_status fk_kv_choose(const fk_kv_cache* cache, const float* mass, const int32_t* pages, int max_pages, const int32_t* lens,
                        int B, int64_t max_len, int keep, int first, int last, int32_t* kept, int32_t* counts, void* ws,

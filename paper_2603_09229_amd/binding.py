@@ -23,7 +23,7 @@ EXPORTS = ("fk_last_error", "fk_workspace_bytes", "fk_assign", "fk_sort_inverse"
            "fk_lloyd_iter", "fk_lloyd_ooc", "fk_ooc_workspace_bytes", "fk_stage_timer_start",
            "fk_stage_timer_stop", "fk_plan", "fk_set_option", "fk_standard_assign",
            "fk_standard_update", "fk_assign_static", "fk_assign_static_limit", "fk_kv_append", "fk_kv_read",
-           "fk_kv_attend", "fk_kv_workspace_bytes", "fk_kv_plan", "fk_kv_attend_tree", "fk_kv_weigh", "fk_kv_choose",
+           "fk_kv_attend", "fk_kv_workspace_bytes", "fk_kv_plan", "fk_kv_attend_tree", "fk_kv_weigh", "fk_kv_weigh_workspace_bytes", "fk_kv_choose",
            "fk_kv_choose_workspace_bytes", "fk_kv_compact")
 STAGES = ("assign", "sort", "reduce", "finalize")
 
@@ -90,7 +90,9 @@ def lib() -> ctypes.CDLL:
         L.fk_kv_attend_tree.restype = i32
         L.fk_kv_attend_tree.argtypes = [cache, vp, i64, i64, i32, i64, vp, i32, vp, vp, i32, i32, i64, f32, i32, vp, i32, vp, vp, vp, sz, vp]
         L.fk_kv_weigh.restype = i32
-        L.fk_kv_weigh.argtypes = [cache, vp, i64, i64, i32, i64, vp, vp, i32, vp, vp, i32, i32, i64, f32, i32, i32, vp, f32, vp, vp, vp]
+        L.fk_kv_weigh.argtypes = [cache, vp, i64, i64, i32, i64, vp, vp, i32, vp, vp, i32, i32, i64, f32, i32, i32, vp, f32, vp, vp, vp, sz, vp]
+        L.fk_kv_weigh_workspace_bytes.restype = sz
+        L.fk_kv_weigh_workspace_bytes.argtypes = [cache, i32, i64, i32, i32, i64]
         L.fk_kv_choose.restype = i32
         L.fk_kv_choose.argtypes = [cache, vp, vp, i32, vp, i32, i64, i32, i32, i32, vp, vp, vp, sz, vp]
         L.fk_kv_choose_workspace_bytes.restype = sz
@@ -546,7 +548,7 @@ def fk_kv_attend_tree(cache: KVCache, q, pages, lens, tree, *, q_start=None, max
 
 
 def fk_kv_weigh(cache: KVCache, q, lse, pages, lens, mass, *, q_start=None, max_q=None, max_len: int = 0, scale=None, causal: bool = True,
-                window: int = 0, known=None, decay: float = 1.0, out=None):
+                window: int = 0, known=None, decay: float = 1.0, ws=None, out=None):
     """The attention weights of q [Tq, q_heads, d], whose softmax sums have the logarithms lse [Tq, q_heads] float32 (fk_kv_attend gives
     them), added up for every token and cache head into mass [pages, heads, page_size] float32, or into `out` beside it.  Tokens from
     place known[b] on ([B] int32) have no weights yet; older ones fade by `decay`.  -> mass, or out"""
@@ -557,11 +559,18 @@ def fk_kv_weigh(cache: KVCache, q, lse, pages, lens, mass, *, q_start=None, max_
     shape = (cache.pages, cache.heads, cache.page_size)
     mp = _array(mass, "mass", cache, torch.float32, shape)
     op = mp if out is None else _array(out, "out", cache, torch.float32, shape)
+    room = max_pages * cache.page_size
+    max_len = min(max_len, room) if max_len > 0 else max_len or room
+    if ws is None:
+        n = lib().fk_kv_weigh_workspace_bytes(ref, heads, Tq, B, max_q, max_len) if max_len > 0 else 0
+        ws = torch.empty(n, dtype=torch.uint8, device=cache.device) if n else None
     _check(lib().fk_kv_weigh(ref, qp, qt, qh, heads, Tq, _array(lse, "lse", cache, torch.float32, (Tq, heads)),
                              _array(pages, "pages", cache, torch.int32, (B, max_pages)), max_pages,
                              _array(lens, "lens", cache, torch.int32, (B,)), qs, B, max_q, max_len,
                              cache.d ** -0.5 if scale is None else scale, causal, window,
-                             0 if known is None else _array(known, "known", cache, torch.int32, (B,)), decay, mp, op, _raw_stream(cache)))
+                             0 if known is None else _array(known, "known", cache, torch.int32, (B,)), decay, mp, op,
+                             0 if ws is None else _array(ws, "ws", cache, torch.uint8, ws.shape), 0 if ws is None else ws.numel(),
+                             _raw_stream(cache)))
     return mass if out is None else out
 
 
@@ -577,10 +586,10 @@ def fk_kv_choose(cache: KVCache, mass, pages, lens, keep: int, *, first: int = 0
         kept = torch.empty((B, cache.heads, max(keep, 0)), dtype=torch.int32, device=cache.device)
     if counts is None:
         counts = torch.empty_like(lens)
-    if not max_len:
-        max_len = max_pages * cache.page_size
+    room = max_pages * cache.page_size
+    max_len = min(max_len, room) if max_len > 0 else max_len or room
     if ws is None:
-        n = L.fk_kv_choose_workspace_bytes(ref, B, max_len)
+        n = L.fk_kv_choose_workspace_bytes(ref, B, max_len) if max_len > 0 else 0
         ws = torch.empty(n, dtype=torch.uint8, device=cache.device) if n else None
     _check(L.fk_kv_choose(ref, _array(mass, "mass", cache, torch.float32, (cache.pages, cache.heads, cache.page_size)),
                           _array(pages, "pages", cache, torch.int32, (B, max_pages)), max_pages,

@@ -18,6 +18,7 @@ struct KVWeigh {
     float decay;
     const float* mass;
     float* out;
+    float* part;          // workspace: sums of divided rows, [B * heads][splits][tokens]
 };
 
 struct KVChoose {
@@ -41,7 +42,11 @@ struct KVWeighPlan {
     int row_waves;        // waves of a workgroup that share its tokens and divide the query rows
     int64_t chunk;        // tokens of a workgroup
     int blocks;           // workgroups along the tokens
+    int splits;           // and along the query rows
 };
+inline size_t weigh_workspace_bytes(const KVWeighPlan& p, int heads, int B) {
+    return p.splits <= 1 ? 0 : align_up((size_t)B * heads * p.splits * p.blocks * p.chunk * sizeof(float), 256);
+}
 KVWeighPlan choose_weigh_plan(const KVView& c, int q_heads, int B, int max_q, int64_t max_len);
 
 fk_status launch_kv_weigh(const KVView& c, const KVWeigh& a, const KVWeighPlan& p, hipStream_t s);

@@ -25,7 +25,7 @@ extern "C" {
 fk_status fk_kv_weigh(const fk_kv_cache* cache, const void* q, int64_t q_token_stride, int64_t q_head_stride, int q_heads, int64_t Tq,
                       const float* lse, const int32_t* pages, int max_pages, const int32_t* lens, const int32_t* q_start, int B, int max_q,
                       int64_t max_len, float scale, int causal, int window, const int32_t* known, float decay, const float* mass,
-                      float* mass_out, void* stream) {
+                      float* mass_out, void* ws, size_t ws_bytes, void* stream) {
     const char* fn = "fk_kv_weigh";
     KVView c;
     fk_status why;
@@ -52,9 +52,28 @@ fk_status fk_kv_weigh(const fk_kv_cache* cache, const void* q, int64_t q_token_s
     if (known) FK_TRY(need(fn, "known", known, 4));
     FK_TRY(need(fn, "mass", mass, 4));
     FK_TRY(need(fn, "mass_out", mass_out, 4));
+    const KVWeighPlan p = choose_weigh_plan(c, q_heads, B, max_q, std::min(max_len, (int64_t)max_pages << c.page_shift));
+    const size_t bytes = weigh_workspace_bytes(p, c.heads, B);
+    if (bytes) FK_TRY(need(fn, "ws", ws, 256));
+    if (ws_bytes < bytes) {
+        set_error("%s: workspace too small: %zu bytes given, %zu needed", fn, ws_bytes, bytes);
+        return FK_EWORKSPACE;
+    }
     const KVWeigh a{{(const uint16_t*)q, q_token_stride, q_head_stride}, q_heads, Tq, lse, pages, lens, q_start, max_pages, B, max_q, scale,
-                    causal != 0, window, known, decay, mass, mass_out};
-    return launch_kv_weigh(c, a, choose_weigh_plan(c, q_heads, B, max_q, std::min(max_len, (int64_t)max_pages << c.page_shift)), (hipStream_t)stream);
+                    causal != 0, window, known, decay, mass, mass_out, (float*)ws};
+    return launch_kv_weigh(c, a, p, (hipStream_t)stream);
+}
+
+size_t fk_kv_weigh_workspace_bytes(const fk_kv_cache* cache, int q_heads, int64_t Tq, int B, int max_q, int64_t max_len) {
+    const char* fn = "fk_kv_weigh_workspace_bytes";
+    KVView c;
+    fk_status why;
+    if (!view_of(fn, cache, false, &c, &why) || check_queries(fn, c, q_heads, Tq, B, max_q, max_len) != FK_OK) return 0;
+    if (max_len < 1) {
+        set_error("%s: max_len must be positive", fn);
+        return 0;
+    }
+    return weigh_workspace_bytes(choose_weigh_plan(c, q_heads, B, max_q, max_len), c.heads, B);
 }
 
 fk_status fk_kv_choose(const fk_kv_cache* cache, const float* mass, const int32_t* pages, int max_pages, const int32_t* lens, int B,

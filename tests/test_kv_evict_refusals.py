@@ -23,7 +23,7 @@ def tree(c=None, **other):
 
 def weigh(c=None, **other):
     return call("fk_kv_weigh", dict(q=P, qt=4096, qh=128, heads=32, Tq=4, lse=P, pages=P, max_pages=3, lens=P, q_start=None, B=4, max_q=1,
-                                    max_len=100, scale=1.0, causal=1, window=0, known=None, decay=1.0, mass=P, out=P), other, c)
+                                    max_len=100, scale=1.0, causal=1, window=0, known=None, decay=1.0, mass=P, out=P, ws=P, room=1 << 30), other, c)
 
 
 def choose(c=None, **other):
@@ -69,6 +69,7 @@ def test_trees_that_are_refused(other, status):
 @pytest.mark.parametrize("other,status", QUERIES + [
     (dict(lse=None), EINVAL), (dict(lse=P + 2), EINVAL), (dict(known=P + 1), EINVAL), (dict(mass=None), EINVAL), (dict(mass=P + 2), EINVAL),
     (dict(out=P + 2), EINVAL), (dict(decay=float("nan")), EINVAL), (dict(decay=float("-inf")), EINVAL), (dict(B=70000, Tq=70000), EUNSUPPORTED),
+    (dict(max_q=1000, Tq=4000, ws=None), EINVAL), (dict(max_q=1000, Tq=4000, ws=P + 128), EINVAL), (dict(max_q=1000, Tq=4000, room=64), EWORKSPACE),
 ])
 def test_weights_that_are_refused(other, status):
     assert weigh(**other) == status
