@@ -6,6 +6,33 @@
 // token; the bits of tokens before the tree count as set, so that a step may begin anywhere.
 #include "fk_kv_attend.h"
 
+namespace fk {
+
+// As for queries in a row, but for the tiles of workgroups that share their rows and do not divide the tokens.  A tree has some dozen query
+// tokens, more rows than one tile, and few sequences leave most of the chip idle: fewer tiles, and more workgroups that each decode the same codes.
+// The cost is the one that choose_kv_plan compares (tenths of a microsecond, steps of 256 tokens).  One tree of 13 tokens, 8 heads of 128,
+// 4 queries each, 700 tokens: three tiles 18.4 us, two 14.6, one 11.6; 8 of 60 over 1500: 53.6, 45.3, 47.1; 10 of 32, 4 heads of 160, 3000 tokens: two
+// 34.3, one 50.9.
+static KVPlan choose_tree_plan(const KVView& c, int q_heads, int B, int max_q, int64_t reach) {
+    KVPlan p = choose_kv_plan(c, q_heads, B, max_q, reach);
+    if (!p.join || p.splits > 1) return p;
+    const int64_t rows = (int64_t)max_q * (q_heads / c.heads), ND = c.d / 32, units = device_cu_count(), steps = cdiv(reach, (int64_t)kJoinWaves * kStep);
+    int64_t least = INT64_MAX;
+    for (int tiles = p.tiles; tiles >= 1; --tiles) {
+        const int64_t blocks = (int64_t)B * c.heads * cdiv(rows, 16 * tiles), more = std::max(blocks - units, (int64_t)0), w = ND * tiles;
+        const int64_t cost = w <= 2 || (tiles == 1 && ND <= 4) ? (40 + 5 * w + (4 + 3 * w) * steps) * units + (15 + w + (7 + 2 * w) * steps) * more
+                                                                : (60 + 2 * w + (10 + 2 * w) * steps) * cdiv(blocks, units) * units;
+        if (cost < least) {
+            least = cost;
+            p.tiles = tiles;
+            p.row_blocks = (int)cdiv(rows, 16 * tiles);
+        }
+    }
+    return p;
+}
+
+}  // namespace fk
+
 using namespace fk;
 
 extern "C" fk_status fk_kv_attend_tree(const fk_kv_cache* cache, const void* q, int64_t q_token_stride, int64_t q_head_stride, int q_heads,
@@ -46,7 +73,7 @@ extern "C" fk_status fk_kv_attend_tree(const fk_kv_cache* cache, const void* q, 
     FK_TRY(need(fn, "out", out, 16));
     if (lse) FK_TRY(need(fn, "lse", lse, 4));
     FK_TRY(need(fn, "ws", ws, 256));
-    const KVPlan p = choose_kv_plan(c, q_heads, B, max_q, reach_of(window, max_q + 1, max_len));
+    const KVPlan p = choose_tree_plan(c, q_heads, B, max_q, reach_of(window, max_q + 1, max_len));
     const size_t bytes = kv_partial_bytes(p, c.d, c.heads, B);
     if (ws_bytes < bytes) {
         set_error("%s: workspace too small: %zu bytes given, %zu needed", fn, ws_bytes, bytes);
