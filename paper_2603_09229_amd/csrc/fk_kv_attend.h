@@ -613,7 +613,7 @@ void kv_attend_kernel(AttendArgs A) {
 #pragma unroll
                 for (int c = 0; c < NT; ++c) X[u][c] = mfma16<BF>(op, Q[c][k], X[u][c]);
             }
-        if constexpr (!JOIN) __builtin_amdgcn_sched_barrier(0);
+        if constexpr (!JOIN || TREE) __builtin_amdgcn_sched_barrier(0);
         in.load_keys(f, row);
 
         float ks[8];
@@ -621,12 +621,12 @@ void kv_attend_kernel(AttendArgs A) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) ks[e] = scale_at<BF>(f.ks[e / 4], e & 3) * A.scale_log2;
         in.load_scales(f, row);
-        if constexpr (!JOIN) __builtin_amdgcn_sched_barrier(0);
+        if constexpr (!JOIN || TREE) __builtin_amdgcn_sched_barrier(0);
         uintx4 w[NT];
         soft.template step<BF, TREE>(X, ks, vs, from + kStep > whole_end || from < whole_from,   // some row does not see all of these tokens
                                seen, from + 4 * q, O, w);
 
-        if constexpr (!JOIN) __builtin_amdgcn_sched_barrier(0);
+        if constexpr (!JOIN || TREE) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int p = 0; p < P::count; ++p) {
             uint32_t pairs[4][2];                                 // [two tokens][half byte]
@@ -648,7 +648,7 @@ void kv_attend_kernel(AttendArgs A) {
                     for (int c = 0; c < NT; ++c) O[s][c] = mfma16<false>(op, w[c], O[s][c]);
                 }
         }
-        if constexpr (!JOIN) __builtin_amdgcn_sched_barrier(0);
+        if constexpr (!JOIN || TREE) __builtin_amdgcn_sched_barrier(0);
         in.load_values(f, row);
     }
 
