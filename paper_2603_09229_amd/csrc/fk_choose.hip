@@ -36,22 +36,24 @@ struct ChooseArgs {
     ChooseState* state;        // [B * heads][parts]
 };
 
-// order of weights as integers; 0 is NaN alone
+// Order of weights as integers.  NaN is 1, below all of them; kNothing is behind the sequence's end and kProtected a place that stays in any
+// case: both are bit patterns of NaN, which no weight's order is.  So nothing but the order decides: the `keep` largest stay.
+constexpr uint32_t kNothing = 0, kProtected = 0xffffffffu;
 __device__ __forceinline__ uint32_t order_of(float w) {
     const uint32_t u = __float_as_uint(w + 0.f);                  // (-0 becomes 0)
-    return w != w ? 0u : u ^ ((uint32_t)((int)u >> 31) | 0x80000000u);
+    return w != w ? 1u : u ^ ((uint32_t)((int)u >> 31) | 0x80000000u);
 }
 
-// Inclusive sum over the lanes of a wave.
-__device__ __forceinline__ int wave_scan(int x, int lane) {
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) {
-        const int y = __shfl_up(x, o);
-        x += lane >= o ? y : 0;
-    }
+// Inclusive sum over the lanes of a wave, without a trip through LDS.
+__device__ __forceinline__ int wave_scan(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);    // within rows of 16: from 1, 2, 4 and 8 lanes below
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);   // the sums of rows 0 and 2 to the rows above them
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);   // and of the lower half to the upper one
     return x;
 }
-
 // How many of the lanes below this one are in the mask.
 __device__ __forceinline__ int lower_lanes(uint64_t mask) {
     return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
@@ -59,30 +61,28 @@ __device__ __forceinline__ int lower_lanes(uint64_t mask) {
 
 struct ChooseShared {
     __align__(16) int bins[kBins][kCopies];
-    int waves[kChooseWaves];
-    int places[32 * kChooseWaves + 64];  // of a round: places that stay for sure, ties times 2^16, per 64 tokens; then before them
+    int waves[kChooseWaves], ties[kChooseWaves];
     ChooseState next;
     int ties_before;
-    int all;
 };
 
-// The bits of the wanted value and what is still wanted below it, from a thread's two counts in descending order; `before_*`: the same counts
+// sums of the waves below this one and of all, from one number a wave
+__device__ __forceinline__ int waves_below(const int* waves, int wave, int lane, int* all) {
+    const int scan = wave_scan(lane < kChooseWaves ? waves[lane] : 0);
+    *all = __builtin_amdgcn_readlane(scan, kChooseWaves - 1);
+    return wave ? __builtin_amdgcn_readlane(scan, wave - 1) : 0;
+}
+
+// The bits of the wanted value and what is still wanted below it, from a thread's two counts in descending order; `earlier`: the same counts
 // in earlier parts.
 __device__ __forceinline__ void find_bin(ChooseShared& S, ChooseState& s, const int (&own)[2], const int (&earlier)[2], int shift, int tid, int* ties_before) {
-    const int lane = tid & 63, wave = tid / 64;
-    const int sum = own[0] + own[1];
-    const int scan = wave_scan(sum, lane);
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid / 64), sum = own[0] + own[1], scan = wave_scan(sum);
     if (lane == 63) S.waves[wave] = scan;
-    if (tid == 0) {
-        S.next = s;
-        S.ties_before = 0;
-    }
     __syncthreads();
-    int above = scan - sum;
-#pragma unroll
-    for (int w = 0; w < kChooseWaves; ++w) above += w < wave ? S.waves[w] : 0;
+    int all;
+    const int below = waves_below(S.waves, wave, lane, &all), above = below + scan - sum;
     const int hit = above < s.missing && s.missing <= above + own[0] ? 0 : above + own[0] < s.missing && s.missing <= above + sum ? 1 : -1;
-    if (hit >= 0) {
+    if (hit >= 0) {                                               // one thread
         S.next.found = s.found | (uint32_t)(kBins - 1 - 2 * tid - hit) << shift;
         S.next.missing = s.missing - above - (hit ? own[0] : 0);
         S.ties_before = earlier[hit];
@@ -93,14 +93,14 @@ __device__ __forceinline__ void find_bin(ChooseShared& S, ChooseState& s, const 
     *ties_before = S.ties_before;
 }
 
-// STAGE -1: everything; 0 to 3: one of four launches over parts.
+// STAGE -1: everything; 0 to 3: one of four launches over parts.  A wave's tokens follow each other, 64 to an item.
 template <int ITEMS, int STAGE>
-__global__ __launch_bounds__(kChooseThreads) void kv_choose_kernel(ChooseArgs A) {
+__global__ __launch_bounds__(kChooseThreads, ITEMS <= 16 ? 8 : 4) void kv_choose_kernel(ChooseArgs A) {
     __shared__ ChooseShared S;
     const KVChoose& a = A.a;
     const KVView& c = A.c;
     const int h = blockIdx.x, b = blockIdx.y, part = STAGE < 0 ? 0 : blockIdx.z, parts = STAGE < 0 ? 1 : A.parts;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid / 64;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid / 64);
     const int len = min(max(a.lens[b], 0), a.max_pages << c.page_shift);
     int32_t* kept = a.kept + ((int64_t)b * c.heads + h) * a.keep;
     if (STAGE <= 0 && h == 0 && part == 0 && tid == 0) a.counts[b] = min(len, a.keep);
@@ -110,34 +110,40 @@ __global__ __launch_bounds__(kChooseThreads) void kv_choose_kernel(ChooseArgs A)
         return;
     }
     const int32_t* table = a.pages + (int64_t)b * a.max_pages;
-    const int from = a.first, to = len - a.last;                  // the middle
     const int each = ((len + parts - 1) / parts + kChooseThreads - 1) / kChooseThreads * kChooseThreads;
-    const int begin = min((int64_t)part * each, (int64_t)len), end = min((int64_t)begin + each, (int64_t)len);
+    const int begin = (int)min((int64_t)part * each, (int64_t)len), end = (int)min((int64_t)begin + each, (int64_t)len);
     const int rounds = (end - begin + ITEMS * kChooseThreads - 1) / (ITEMS * kChooseThreads);
 
     uint32_t v[ITEMS];
+    auto first_of = [&](int round) { return begin + (round * kChooseWaves + wave) * (ITEMS * 64) + lane; };
     auto load = [&](int round) {
+        const int t0 = first_of(round);
         int page[ITEMS];
-        const int t0 = begin + round * (ITEMS * kChooseThreads) + tid;
 #pragma unroll
-        for (int i = 0; i < ITEMS; ++i) page[i] = table[min(t0 + i * kChooseThreads, len - 1) >> c.page_shift];
+        for (int i = 0; i < ITEMS; ++i) page[i] = table[min(t0 + i * 64, len - 1) >> c.page_shift];
+        float w[ITEMS];
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
-            const int t = min(t0 + i * kChooseThreads, len - 1);
-            page[i] = min(max(page[i], 0), (int)c.pages - 1);
-            v[i] = order_of(a.mass[(((int64_t)page[i] * c.heads + h) << c.page_shift) + (t & ((1 << c.page_shift) - 1))]);
+            const int t = min(t0 + i * 64, len - 1), p = min(max(page[i], 0), (int)c.pages - 1);
+            w[i] = a.mass[(((int64_t)p * c.heads + h) << c.page_shift) + (t & ((1 << c.page_shift) - 1))];
+        }
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const int t = t0 + i * 64;
+            v[i] = t >= end ? kNothing : t < a.first || t >= len - a.last ? kProtected : order_of(w[i]);
         }
     };
-    auto middle = [&](int t) { return t >= from && t < min(to, end); };
+    auto clear = [&] {
+#pragma unroll
+        for (int i = 0; i < kBins * kCopies / 4 / kChooseThreads; ++i) ((uintx4*)S.bins)[i * kChooseThreads + tid] = uintx4{0, 0, 0, 0};
+    };
+    // (the counts are cleared: by `clear`, or by who read them last)
     auto count = [&](const ChooseState& s, int shift, int bits) {
-        for (int i = tid; i < kBins * kCopies / 4; i += kChooseThreads) ((uintx4*)S.bins)[i] = uintx4{0, 0, 0, 0};
-        __syncthreads();
         for (int r = 0; r < rounds; ++r) {
-            if (rounds > 1 || STAGE >= 0 || shift == 21) load(r);
-            const int t0 = begin + r * (ITEMS * kChooseThreads) + tid;
+            if (rounds > 1 || STAGE >= 0) load(r);
 #pragma unroll
             for (int i = 0; i < ITEMS; ++i)
-                if (middle(t0 + i * kChooseThreads) && (shift == 21 || (v[i] ^ s.found) >> (shift + bits) == 0))
+                if (shift == 21 || (v[i] ^ s.found) >> (shift + bits) == 0)
                     atomicAdd(&S.bins[v[i] >> shift & ((1 << bits) - 1)][lane & (kCopies - 1)], 1);
         }
         __syncthreads();
@@ -146,30 +152,38 @@ __global__ __launch_bounds__(kChooseThreads) void kv_choose_kernel(ChooseArgs A)
     auto counted = [&](int (&own)[2]) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const uintx4 x = *(const uintx4*)S.bins[kBins - 1 - 2 * tid - i];
+            uintx4& at = *(uintx4*)S.bins[kBins - 1 - 2 * tid - i];
+            const uintx4 x = at;
+            if (STAGE < 0) at = uintx4{0, 0, 0, 0};
             own[i] = (int)(x[0] + x[1] + x[2] + x[3]);
         }
     };
 
     constexpr int shifts[3] = {21, 10, 0}, widths[3] = {11, 11, 10};
-    ChooseState s{0, a.keep - a.first - a.last, 0};
+    ChooseState s{0, a.keep, 0};
     int ties_before = 0;
     if constexpr (STAGE < 0) {
         const int none[2] = {0, 0};
-#pragma unroll
-        for (int p = 0; p < 3; ++p) {
-            count(s, shifts[p], widths[p]);
+        clear();
+        if (rounds == 1) load(0);
+        __syncthreads();
+        auto pass = [&](int shift, int bits) {
+            count(s, shift, bits);
             int own[2];
             counted(own);
-            find_bin(S, s, own, none, shifts[p], tid, &ties_before);
-        }
+            find_bin(S, s, own, none, shift, tid, &ties_before);
+        };
+        pass(shifts[0], widths[0]);
+#pragma unroll 1
+        for (int p = 1; p < 3; ++p) pass(p == 1 ? shifts[1] : shifts[2], p == 1 ? widths[1] : widths[2]);
     } else {
+        typedef int intx2 __attribute__((ext_vector_type(2)));
         const int64_t unit = (int64_t)b * c.heads + h, stage_ints = (int64_t)a.B * c.heads * parts * kBins;
         ChooseState* mine = A.state + unit * parts + part;
+        if constexpr (STAGE < 3) clear();
         if constexpr (STAGE > 0) {
             if (STAGE > 1) s = *mine;
             const int* all = A.counts + ((STAGE - 1) & 1) * stage_ints + unit * parts * kBins + (kBins - 2 - 2 * tid);
-            typedef int intx2 __attribute__((ext_vector_type(2)));
             int own[2] = {0, 0}, earlier[2] = {0, 0};
 #pragma unroll 8
             for (int p = 0; p < parts; ++p) {
@@ -181,76 +195,56 @@ __global__ __launch_bounds__(kChooseThreads) void kv_choose_kernel(ChooseArgs A)
             }
             find_bin(S, s, own, earlier, shifts[STAGE - 1], tid, &ties_before);
             // places that stay in earlier parts: those above the bits found
-            const uint32_t bin = (s.found >> shifts[STAGE - 1]) & ((1u << widths[STAGE - 1]) - 1);
-            const uint32_t bin0 = kBins - 1 - 2 * tid;
-            int above = (bin0 > bin ? earlier[0] : 0) + (bin0 - 1 > bin && tid < kBins / 2 ? earlier[1] : 0);
-            above = wave_scan(above, lane);
+            const uint32_t bin = (s.found >> shifts[STAGE - 1]) & ((1u << widths[STAGE - 1]) - 1), bin0 = kBins - 1 - 2 * tid;
+            const int above = wave_scan((bin0 > bin ? earlier[0] : 0) + (bin0 > bin + 1 ? earlier[1] : 0));
+            if (lane == 63) S.ties[wave] = above;
             __syncthreads();
-            if (lane == 63) S.waves[wave] = above;
-            __syncthreads();
-#pragma unroll
-            for (int w = 0; w < kChooseWaves; ++w) s.before += S.waves[w];
-            __syncthreads();
+            int sum;
+            waves_below(S.ties, wave, lane, &sum);
+            s.before += sum;
         }
         if constexpr (STAGE < 3) {
+            __syncthreads();                                      // (cleared)
             count(s, shifts[STAGE], widths[STAGE]);
             int own[2];
             counted(own);
-            typedef int intx2 __attribute__((ext_vector_type(2)));
             *(intx2*)(A.counts + (STAGE & 1) * stage_ints + (unit * parts + part) * kBins + (kBins - 2 - 2 * tid)) = intx2{own[1], own[0]};
             if (STAGE > 0 && tid == 0) *mine = s;
             return;
         }
+        __syncthreads();
     }
 
-    const bool some = a.keep > a.first + a.last;
-    const int ties = s.missing;
-    // places that stay before this part: protected ones, larger ones, and the ties that found room
-    int done = min(begin, from) + max(begin - max(to, 0), 0) + (some ? s.before : 0), tied = ties_before;
+    // Places that stay before this part, and ties that found room in it or earlier.
+    int done = s.before, tied = ties_before;
     for (int r = 0; r < rounds; ++r) {
         if (rounds > 1 || STAGE >= 0) load(r);
-        const int t0 = begin + r * (ITEMS * kChooseThreads) + tid;
-        auto more = [&](int i) {
-            const int t = t0 + i * kChooseThreads;
-            return (t < end && (t < from || t >= to)) || (some && middle(t) && v[i] > s.found);
-        };
-        auto tie = [&](int i) { return some && middle(t0 + i * kChooseThreads) && v[i] == s.found; };
+        int mores = 0, same = 0;
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
-            const int x = __popcll(__ballot(more(i))) + (__popcll(__ballot(tie(i))) << 16);
-            if (lane == 0) S.places[i * kChooseWaves + wave] = x;
+            mores += __popcll(__ballot(v[i] > s.found));
+            same += __popcll(__ballot(v[i] == s.found));
+        }
+        if (r) __syncthreads();                                   // (the last round's sums are read)
+        if (lane == 0) {
+            S.waves[wave] = mores;
+            S.ties[wave] = same;
         }
         __syncthreads();
-        constexpr int ENTRIES = ITEMS * kChooseWaves;             // at most 512, by one wave
-        if (wave == 0) {
-            constexpr int EACH = (ENTRIES + 63) / 64;
-            int x[EACH], sum = 0;
-#pragma unroll
-            for (int k = 0; k < EACH; ++k) {
-                x[k] = lane * EACH + k < ENTRIES ? S.places[lane * EACH + k] : 0;
-                sum += x[k];
-            }
-            int at = wave_scan(sum, lane);
-            if (lane == 63) S.all = at;
-            at -= sum;
-#pragma unroll
-            for (int k = 0; k < EACH; ++k) {
-                S.places[lane * EACH + k] = at;
-                at += x[k];
-            }
-        }
-        __syncthreads();
+        int all, all_ties;
+        int at = done + waves_below(S.waves, wave, lane, &all), met = tied + waves_below(S.ties, wave, lane, &all_ties);
+        const int t0 = first_of(r);
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
-            const int x = S.places[i * kChooseWaves + wave];
-            const bool stays = more(i), equal = tie(i);
-            const int met = tied + (int)((uint32_t)x >> 16) + lower_lanes(__ballot(equal));
-            if (stays || (equal && met < ties)) kept[done + (x & 0xffff) + lower_lanes(__ballot(stays)) + min(met, ties)] = t0 + i * kChooseThreads;
+            const bool more = v[i] > s.found, tie = v[i] == s.found;
+            const uint64_t m = __ballot(more), e = __ballot(tie);
+            const int here = met + lower_lanes(e);
+            if (more || (tie && here < s.missing)) kept[at + lower_lanes(m) + min(here, s.missing)] = t0 + i * 64;
+            at += __popcll(m);
+            met += __popcll(e);
         }
-        const int all = S.all;
-        done += all & 0xffff;
-        tied += (int)((uint32_t)all >> 16);
-        __syncthreads();
+        done += all;
+        tied += all_ties;
     }
 }
 
