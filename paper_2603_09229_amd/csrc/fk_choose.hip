@@ -7,6 +7,11 @@
 //
 // A workgroup holds the weights of a sequence and head in registers, read once.  Sequences of more than kWhole tokens are divided among
 // workgroups, and the four steps are launches of their own: each counts its part, the next one adds the parts' counts up.
+//
+// What bounds it: latency, of the page and the weight behind each other, of three rounds of counting with three barriers each, and of the
+// places' prefix sums.  8 heads: one sequence of 1100 tokens 6.5 us, 64 of up to 8192 13.6 (15 MB, 1.1 TB/s; counted one weight a thread at a time from memory
+// 29), one of 131072 in 16 parts FIGURE (in one workgroup 299).  Counts are held four times: weights are bell-shaped or worse, and lanes with the
+// same leading bits wait for each other.  Sums within a wave go by DPP, six instructions instead of six trips through LDS.
 #include <algorithm>
 
 #include "fk_device.h"
@@ -140,7 +145,7 @@ __global__ __launch_bounds__(kChooseThreads, ITEMS <= 16 ? 8 : 4) void kv_choose
     // (the counts are cleared: by `clear`, or by who read them last)
     auto count = [&](const ChooseState& s, int shift, int bits) {
         for (int r = 0; r < rounds; ++r) {
-            if (rounds > 1 || STAGE >= 0) load(r);
+            if (rounds > 1) load(r);
 #pragma unroll
             for (int i = 0; i < ITEMS; ++i)
                 if (shift == 21 || (v[i] ^ s.found) >> (shift + bits) == 0)
@@ -162,10 +167,10 @@ __global__ __launch_bounds__(kChooseThreads, ITEMS <= 16 ? 8 : 4) void kv_choose
     constexpr int shifts[3] = {21, 10, 0}, widths[3] = {11, 11, 10};
     ChooseState s{0, a.keep, 0};
     int ties_before = 0;
+    if (rounds == 1) load(0);                                     // (on its way while counts are cleared or added up)
+    if constexpr (STAGE < 3) clear();
     if constexpr (STAGE < 0) {
         const int none[2] = {0, 0};
-        clear();
-        if (rounds == 1) load(0);
         __syncthreads();
         auto pass = [&](int shift, int bits) {
             count(s, shift, bits);
@@ -180,7 +185,6 @@ __global__ __launch_bounds__(kChooseThreads, ITEMS <= 16 ? 8 : 4) void kv_choose
         typedef int intx2 __attribute__((ext_vector_type(2)));
         const int64_t unit = (int64_t)b * c.heads + h, stage_ints = (int64_t)a.B * c.heads * parts * kBins;
         ChooseState* mine = A.state + unit * parts + part;
-        if constexpr (STAGE < 3) clear();
         if constexpr (STAGE > 0) {
             if (STAGE > 1) s = *mine;
             const int* all = A.counts + ((STAGE - 1) & 1) * stage_ints + unit * parts * kBins + (kBins - 2 - 2 * tid);
@@ -218,7 +222,7 @@ __global__ __launch_bounds__(kChooseThreads, ITEMS <= 16 ? 8 : 4) void kv_choose
     // Places that stay before this part, and ties that found room in it or earlier.
     int done = s.before, tied = ties_before;
     for (int r = 0; r < rounds; ++r) {
-        if (rounds > 1 || STAGE >= 0) load(r);
+        if (rounds > 1) load(r);
         int mores = 0, same = 0;
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
