@@ -399,7 +399,7 @@ fk_status fk_kv_attend_tree(const fk_kv_cache* cache, const void* q, int64_t q_t
  *   known            device, [B] int32, or NULL: tokens from place known[b] on have no weights yet, and what mass holds of them is not
  *                    read.  lens[b] less the new tokens for a decoding step, 0 for a prompt; NULL: all have.
  *   decay            finite; 1 adds up, less than 1 lets older weights fade
- * The other arguments are those of fk_kv_attend; the keys of the cache are read, its values are not.  No sum depends on the order of
+ * A token whose page is outside the cache is left out.  The other arguments are those of fk_kv_attend; the keys of the cache are read, its values are not.  No sum depends on the order of
  * workgroups.  A page belongs to one sequence of a call (two would write its weights at once).  A key that is not finite has the weight NaN if a query sees it.
  */
 fk_status fk_kv_weigh(const fk_kv_cache* cache, const void* q, int64_t q_token_stride, int64_t q_head_stride, int q_heads,

@@ -482,6 +482,13 @@ def fk_kv_plan(cache: KVCache, B: int, q_heads: int, max_q: int, max_len: int, w
     return buf.value.decode()
 
 
+_EWORKSPACE = 3
+
+
+def _workspace(cache: KVCache, n: int) -> torch.Tensor:
+    return torch.empty(n, dtype=torch.uint8, device=cache.device)
+
+
 def _queries(cache: KVCache, q, pages, q_start, max_q, window):
     """What the queries' arguments come to -> (B, max_pages, pointer of q_start, max_q, window)."""
     B, max_pages = pages.shape
@@ -559,18 +566,20 @@ def fk_kv_weigh(cache: KVCache, q, lse, pages, lens, mass, *, q_start=None, max_
     shape = (cache.pages, cache.heads, cache.page_size)
     mp = _array(mass, "mass", cache, torch.float32, shape)
     op = mp if out is None else _array(out, "out", cache, torch.float32, shape)
-    room = max_pages * cache.page_size
-    max_len = min(max_len, room) if max_len > 0 else max_len or room
-    if ws is None:
-        n = lib().fk_kv_weigh_workspace_bytes(ref, heads, Tq, B, max_q, max_len) if max_len > 0 else 0
-        ws = torch.empty(n, dtype=torch.uint8, device=cache.device) if n else None
-    _check(lib().fk_kv_weigh(ref, qp, qt, qh, heads, Tq, _array(lse, "lse", cache, torch.float32, (Tq, heads)),
-                             _array(pages, "pages", cache, torch.int32, (B, max_pages)), max_pages,
-                             _array(lens, "lens", cache, torch.int32, (B,)), qs, B, max_q, max_len,
-                             cache.d ** -0.5 if scale is None else scale, causal, window,
-                             0 if known is None else _array(known, "known", cache, torch.int32, (B,)), decay, mp, op,
-                             0 if ws is None else _array(ws, "ws", cache, torch.uint8, ws.shape), 0 if ws is None else ws.numel(),
-                             _raw_stream(cache)))
+    L = lib()
+    args = (ref, qp, qt, qh, heads, Tq, _array(lse, "lse", cache, torch.float32, (Tq, heads)),
+            _array(pages, "pages", cache, torch.int32, (B, max_pages)), max_pages, _array(lens, "lens", cache, torch.int32, (B,)), qs, B, max_q,
+            max_len, cache.d ** -0.5 if scale is None else scale, causal, window,
+            0 if known is None else _array(known, "known", cache, torch.int32, (B,)), decay, mp, op)
+    if ws is not None:
+        _check(L.fk_kv_weigh(*args, _array(ws, "ws", cache, torch.uint8, ws.shape), ws.numel(), _raw_stream(cache)))
+    else:
+        status = L.fk_kv_weigh(*args, 0, 0, _raw_stream(cache))       # few queries need no workspace, and their calls are the short ones
+        if status == _EWORKSPACE:
+            room = max_pages * cache.page_size
+            ws = _workspace(cache, L.fk_kv_weigh_workspace_bytes(ref, heads, Tq, B, max_q, min(max_len or room, room)))
+            status = L.fk_kv_weigh(*args, ws.data_ptr(), ws.numel(), _raw_stream(cache))
+        _check(status)
     return mass if out is None else out
 
 
@@ -586,18 +595,18 @@ def fk_kv_choose(cache: KVCache, mass, pages, lens, keep: int, *, first: int = 0
         kept = torch.empty((B, cache.heads, max(keep, 0)), dtype=torch.int32, device=cache.device)
     if counts is None:
         counts = torch.empty_like(lens)
-    room = max_pages * cache.page_size
-    max_len = min(max_len, room) if max_len > 0 else max_len or room
-    if ws is None:
-        n = L.fk_kv_choose_workspace_bytes(ref, B, max_len) if max_len > 0 else 0
-        ws = torch.empty(n, dtype=torch.uint8, device=cache.device) if n else None
-    _check(L.fk_kv_choose(ref, _array(mass, "mass", cache, torch.float32, (cache.pages, cache.heads, cache.page_size)),
-                          _array(pages, "pages", cache, torch.int32, (B, max_pages)), max_pages,
-                          _array(lens, "lens", cache, torch.int32, (B,)), B, max_len, keep, first, last,
-                          _array(kept, "kept", cache, torch.int32, (B, cache.heads, keep)),
-                          _array(counts, "counts", cache, torch.int32, (B,)),
-                          0 if ws is None else _array(ws, "ws", cache, torch.uint8, ws.shape), 0 if ws is None else ws.numel(),
-                          _raw_stream(cache)))
+    args = (ref, _array(mass, "mass", cache, torch.float32, (cache.pages, cache.heads, cache.page_size)),
+            _array(pages, "pages", cache, torch.int32, (B, max_pages)), max_pages, _array(lens, "lens", cache, torch.int32, (B,)), B, max_len, keep,
+            first, last, _array(kept, "kept", cache, torch.int32, (B, cache.heads, keep)), _array(counts, "counts", cache, torch.int32, (B,)))
+    if ws is not None:
+        _check(L.fk_kv_choose(*args, _array(ws, "ws", cache, torch.uint8, ws.shape), ws.numel(), _raw_stream(cache)))
+    else:
+        status = L.fk_kv_choose(*args, 0, 0, _raw_stream(cache))      # (as in fk_kv_weigh)
+        if status == _EWORKSPACE:
+            room = max_pages * cache.page_size
+            ws = _workspace(cache, L.fk_kv_choose_workspace_bytes(ref, B, min(max_len or room, room)))
+            status = L.fk_kv_choose(*args, ws.data_ptr(), ws.numel(), _raw_stream(cache))
+        _check(status)
     return kept, counts
 
 

@@ -10,7 +10,7 @@
 //
 // What bounds it: latency, of the page and the weight behind each other, of three rounds of counting with three barriers each, and of the
 // places' prefix sums.  8 heads: one sequence of 1100 tokens 6.5 us, 64 of up to 8192 13.6 (15 MB, 1.1 TB/s; counted one weight a thread at a time from memory
-// 29), one of 131072 in 16 parts FIGURE (in one workgroup 299).  Counts are held four times: weights are bell-shaped or worse, and lanes with the
+// 29), one of 131072 in 16 parts 23.8 (in one workgroup 299).  Counts are held four times: weights are bell-shaped or worse, and lanes with the
 // same leading bits wait for each other.  Sums within a wave go by DPP, six instructions instead of six trips through LDS.
 #include <algorithm>
 
@@ -20,7 +20,9 @@
 namespace fk {
 
 constexpr int kChooseThreads = 1024, kChooseWaves = kChooseThreads / 64;
-constexpr int kWhole = 32 * kChooseThreads;   // most tokens that one workgroup holds in registers
+// Most tokens that one workgroup holds in registers.  8 heads of one sequence: 9000 tokens 13.7 us; 32 a thread no longer fit, 32000 tokens 54, and 33000 in
+// parts 22.
+constexpr int kWhole = 16 * kChooseThreads;
 constexpr int kPart = 8 * kChooseThreads;     // fewest of a part
 constexpr int kMostParts = 64;
 constexpr int kBins = 2048;
@@ -100,7 +102,7 @@ __device__ __forceinline__ void find_bin(ChooseShared& S, ChooseState& s, const 
 
 // STAGE -1: everything; 0 to 3: one of four launches over parts.  A wave's tokens follow each other, 64 to an item.
 template <int ITEMS, int STAGE>
-__global__ __launch_bounds__(kChooseThreads, ITEMS <= 16 ? 8 : 4) void kv_choose_kernel(ChooseArgs A) {
+__global__ __launch_bounds__(kChooseThreads, 8) void kv_choose_kernel(ChooseArgs A) {
     __shared__ ChooseShared S;
     const KVChoose& a = A.a;
     const KVView& c = A.c;
@@ -279,10 +281,8 @@ fk_status launch_kv_choose(const KVView& c, const KVChoose& a, int64_t max_len, 
         kv_choose_kernel<4, -1><<<grid, kChooseThreads, 0, s>>>(A);
     } else if (max_len <= 8 * kChooseThreads) {
         kv_choose_kernel<8, -1><<<grid, kChooseThreads, 0, s>>>(A);
-    } else if (max_len <= 16 * kChooseThreads) {
+    } else {                                                      // (longer ones, where there are enough of them, in turns)
         kv_choose_kernel<16, -1><<<grid, kChooseThreads, 0, s>>>(A);
-    } else {
-        kv_choose_kernel<32, -1><<<grid, kChooseThreads, 0, s>>>(A);
     }
     FK_HIP(hipGetLastError());
     return FK_OK;

@@ -54,11 +54,11 @@ fk_status fk_kv_weigh(const fk_kv_cache* cache, const void* q, int64_t q_token_s
     FK_TRY(need(fn, "mass_out", mass_out, 4));
     const KVWeighPlan p = choose_weigh_plan(c, q_heads, B, max_q, std::min(max_len, (int64_t)max_pages << c.page_shift));
     const size_t bytes = weigh_workspace_bytes(p, c.heads, B);
-    if (bytes) FK_TRY(need(fn, "ws", ws, 256));
     if (ws_bytes < bytes) {
         set_error("%s: workspace too small: %zu bytes given, %zu needed", fn, ws_bytes, bytes);
         return FK_EWORKSPACE;
     }
+    if (bytes) FK_TRY(need(fn, "ws", ws, 256));
     const KVWeigh a{{(const uint16_t*)q, q_token_stride, q_head_stride}, q_heads, Tq, lse, pages, lens, q_start, max_pages, B, max_q, scale,
                     causal != 0, window, known, decay, mass, mass_out, (float*)ws};
     return launch_kv_weigh(c, a, p, (hipStream_t)stream);
@@ -100,11 +100,11 @@ fk_status fk_kv_choose(const fk_kv_cache* cache, const float* mass, const int32_
     FK_TRY(need(fn, "counts", counts, 4));
     max_len = max_len ? std::min(max_len, room) : room;
     const size_t bytes = choose_workspace_bytes(c, B, max_len);
-    if (bytes) FK_TRY(need(fn, "ws", ws, 256));
     if (ws_bytes < bytes) {
         set_error("%s: workspace too small: %zu bytes given, %zu needed", fn, ws_bytes, bytes);
         return FK_EWORKSPACE;
     }
+    if (bytes) FK_TRY(need(fn, "ws", ws, 256));
     const KVChoose a{mass, pages, lens, max_pages, B, keep, first, last, kept, counts};
     return launch_kv_choose(c, a, max_len, ws, (hipStream_t)stream);
 }

@@ -132,12 +132,14 @@ __global__ __launch_bounds__(kWeighThreads, !STREAM && ND <= 4 ? 4 : 2) void kv_
     const int32_t* table = a.pages + (int64_t)b * a.max_pages;
     const int last = (a.max_pages << c.page_shift) - 1;
     int page;
+    bool inside;                                                  // whether that page is one of the cache's: otherwise nothing is written
     uint32_t codes[PARTS][ND];
     uint16_t scale;
     float old;
     int64_t at;                                                   // the cache's row of token t0 + lane
     auto ask_page = [&](int t0) { page = table[min(t0 + lane, last) >> c.page_shift]; };
     auto ask = [&](int t0) {
+        inside = page >= 0 && page < c.pages;
         page = min(max(page, 0), (int)c.pages - 1);
 #pragma unroll
         for (int u = 0; u < PARTS; ++u) {
@@ -148,7 +150,7 @@ __global__ __launch_bounds__(kWeighThreads, !STREAM && ND <= 4 ? 4 : 2) void kv_
         }
         at = (((int64_t)page * c.heads + h) << c.page_shift) + (min(t0 + lane, last) & ((1 << c.page_shift) - 1));
         scale = c.k_scale[at];
-        old = t0 + lane < min(known, end) ? a.mass[at] : 0.f;
+        old = inside && t0 + lane < min(known, end) ? a.mass[at] : 0.f;
     };
     ask_page(begin + token_wave * TOKENS);
 
@@ -235,7 +237,7 @@ __global__ __launch_bounds__(kWeighThreads, !STREAM && ND <= 4 ? 4 : 2) void kv_
         const int t0 = step + token_wave * TOKENS;
         const bool some = t0 < end, divided = STREAM && A.splits > 1 && step < A.bound;
         if (STREAM && !divided && split) break;                   // (tokens behind the bound that the call names are not divided)
-        const int64_t to = at;
+        const int64_t to = inside ? at : -1;
         const float was = old;
         float acc[4] = {0, 0, 0, 0}, ks[4];
         // the scales of tokens 16 u + n
@@ -398,7 +400,7 @@ __global__ __launch_bounds__(kWeighThreads, !STREAM && ND <= 4 ? 4 : 2) void kv_
         }
         if (row_wave || lane >= TOKENS || t0 + lane >= end) continue;
         if (divided) A.a.part[((int64_t)unit * A.splits + split) * A.bound + t0 + lane] = sum;
-        else a.out[to] = t0 + lane < known ? fmaf(a.decay, was, sum) : sum;
+        else if (to >= 0) a.out[to] = t0 + lane < known ? fmaf(a.decay, was, sum) : sum;
     }
 }
 
@@ -410,7 +412,8 @@ __global__ __launch_bounds__(256) void kv_weigh_join_kernel(WeighArgs A) {
     const int64_t t = (int64_t)(blockIdx.x / units) * 256 + threadIdx.x;
     const int len = min(max(a.lens[b], 0), a.max_pages << c.page_shift);
     if (t >= min((int64_t)len, A.bound)) return;
-    const int page = min(max(a.pages[(int64_t)b * a.max_pages + (t >> c.page_shift)], 0), (int)c.pages - 1);
+    const int page = a.pages[(int64_t)b * a.max_pages + (t >> c.page_shift)];
+    if (page < 0 || page >= c.pages) return;
     const int64_t at = (((int64_t)page * c.heads + h) << c.page_shift) + (t & ((1 << c.page_shift) - 1));
     const float* part = a.part + (int64_t)unit * A.splits * A.bound + t;
     float sum = 0.f;
@@ -465,7 +468,7 @@ static fk_status launch_weigh(const WeighArgs& A, const KVWeighPlan& p, hipStrea
 
 fk_status launch_kv_weigh(const KVView& c, const KVWeigh& a, const KVWeighPlan& p, hipStream_t s) {
     const int64_t units = (int64_t)c.heads * a.B, bound = p.blocks * p.chunk;
-    if (p.blocks * p.splits * units > INT32_MAX / kWeighThreads) {
+    if (p.blocks * p.splits * units > UINT32_MAX / kWeighThreads) {
         set_error("fk_kv_weigh: unsupported size: %lld workgroups", (long long)(p.blocks * p.splits * units));
         return FK_EUNSUPPORTED;
     }

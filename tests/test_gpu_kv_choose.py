@@ -100,6 +100,9 @@ def test_very_long_sequences_by_their_sorted_weights():
                                        last=500, max_len=L)
         order = flat[:, 10:L - 500].sort(dim=1, descending=True, stable=True).indices[:, :keep - 510] + 10
         want = torch.cat([torch.arange(10).expand(2, 10), order, torch.arange(L - 500, L).expand(2, 500)], dim=1).sort(dim=1).values
+        short = fk.fk_kv_choose(cache, mass.to(DEV), table.to(DEV), torch.tensor([L], dtype=torch.int32, device=DEV), keep, first=10, last=500,
+                                max_len=40000)                    # a wrong bound: fewer parts, each in several rounds
+        assert torch.equal(short[0], kept)
         assert torch.equal(kept[0].cpu(), want.int()) and counts.item() == keep
 
 

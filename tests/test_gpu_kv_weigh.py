@@ -118,6 +118,23 @@ def test_a_wrong_upper_bound_of_the_lengths_costs_time_only():
     run(F16, [9000, 100], [1, 1], 1, 8, 64, 64, seed=8, max_len=1 << 20)
 
 
+@pytest.mark.parametrize("n", [1, 300])
+def test_tokens_whose_page_is_outside_the_cache_are_left_out(n):
+    cache, q, table, starts = make(F16, [700, 400], [n, n], 2, 4, 64, 64, 3)
+    k = kv_plain.values(cache.k_codes, cache.k_scale, cache.k_levels)
+    sees = [plain.row_sees(L, n, True, 0) for L in (700, 400)]
+    lse = plain.attend(k, k, q, table, [700, 400], starts, 0.125, sees)[1].float()
+    mass = torch.rand(cache.pages, 2, 64, device=DEV)
+    want, bound = plain.weigh(k, q, lse, table, [700, 400], starts, 0.125, sees, [700, 400], 1.0, mass, mass)
+    wild, was = table.clone(), mass.clone()
+    for b, p, page in ((0, 1, -1), (0, 8, cache.pages), (1, 0, 2 ** 31 - 1), (1, 3, -2 ** 31)):
+        rows = table[b, p].long()
+        want[rows], bound[rows] = was[rows].double(), 0.0
+        wild[b, p] = page
+    fk.fk_kv_weigh(cache, q, lse, wild, ints([700, 400]), mass, max_q=n)
+    assert ((mass.double() - want).abs() <= bound).all()
+
+
 def small(seed=13, n=40, L=200):
     cache, q, table, starts = make(F16, [L], [n], 1, 2, 64, 16, seed)
     lens = ints([L])

@@ -75,6 +75,11 @@ def test_weights_that_are_refused(other, status):
     assert weigh(**other) == status
 
 
+def test_more_workgroups_than_a_launch_has():
+    big = cache(heads=256, d=32)
+    assert weigh(big, heads=256, B=65535, Tq=65535, max_pages=1 << 20, max_len=1 << 20) == EUNSUPPORTED and b"workgroups" in fk.lib().fk_last_error()
+
+
 @pytest.mark.parametrize("other,status", [
     (dict(keep=0), EINVAL), (dict(keep=-5), EINVAL), (dict(first=-1), EINVAL), (dict(last=-1), EINVAL), (dict(first=41), EINVAL),
     (dict(first=2 ** 31 - 1, last=2 ** 31 - 1), EINVAL), (dict(max_len=-1), EINVAL), (dict(B=0), EINVAL), (dict(B=70000), EUNSUPPORTED),
