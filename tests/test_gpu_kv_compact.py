@@ -81,6 +81,27 @@ def test_one_row_is_dropped_and_all_behind_it_move():
     check(cache, mass, table, kept, [2999], [0], None)
 
 
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("share", [0.1, 0.5, 0.95])
+def test_long_sequences_in_place(d, share):
+    """More rows than a tile: those from behind what is written, and those that are moved in order."""
+    lens = [9000, 5000]
+    cache, table, mass, _, g = make([L + 30 for L in lens], 2, d, 64, int(d + 10 * share))
+    keep = [int(L * share) for L in lens]
+    check(cache, mass, table, places(lens, keep, 2, g), keep, [0, 0], None)
+    kept = places(lens, keep, 2, g)
+    kept[:, :, 5::7] = -1                                         # places that are left out
+    check(cache, mass, table, kept, keep, [30, 17], None)
+
+
+def test_the_first_and_the_last_tokens_of_long_sequences_in_place():
+    cache, table, mass, _, _ = make([20000], 2, 64, 64, 9)
+    kept = torch.cat([torch.arange(4), torch.arange(20000 - 8000, 20000)]).int().view(1, 1, -1)
+    check(cache, mass, table, kept, [8004], [0], None)
+    kept = torch.cat([torch.arange(4), torch.arange(20000 - 18000, 20000)]).int().view(1, 1, -1)
+    check(cache, mass, table, kept, [18004], [0], None)
+
+
 def test_a_branch_behind_a_prefix():
     cache, table, mass, _, _ = make([150, 40, 20], 4, 64, 16, 4)
     kept = torch.tensor([[0, 3, 7, 11], [2, 3, -1, -1], [0, 1, 2, 9]], dtype=torch.int32)[:, None]
