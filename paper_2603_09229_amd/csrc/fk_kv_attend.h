@@ -109,6 +109,7 @@ struct AttendArgs {
     int chunk;
     float scale_log2;          // positive, so that scores that are not seen stay -inf:
     uint32_t flip;             // the signs of the queries' channels are flipped instead
+    bool longest_first = false;   // trees: which sequence comes when
 };
 
 // Blocks of the values' channels by the number of bytes that a lane takes of each: ND bytes in pieces of 4, 2 and 1 (powers of two, so
@@ -370,6 +371,17 @@ __device__ __forceinline__ float lse_of(float top, float sum) {
     return sum > 0.f || sum != sum ? (top + __log2f(sum)) * 0.6931471805599453f : -INFINITY;
 }
 
+// The sequence that is longer than `rank` others (of equal ones the later), of up to 64.
+__device__ __forceinline__ int of_rank(const int32_t* lens, int B, int rank, int lane) {
+    const int mine = lane < B ? lens[lane] : INT32_MIN;
+    int longer = lane < B ? 0 : B;
+    for (int j = 0; j < B; ++j) {
+        const int other = __builtin_amdgcn_readlane(mine, j);
+        longer += other > mine || (other == mine && j < lane) ? 1 : 0;
+    }
+    return __ffsll((unsigned long long)__ballot(longer == rank)) - 1;
+}
+
 // References and sums of a wave's rows; a lane keeps its column's, its own tokens' share of the sum.
 template <int NT, int S>
 struct Softmax {
@@ -527,6 +539,8 @@ void kv_attend_kernel(AttendArgs A) {
     const bool packed = !JOIN && A.row_blocks < WAVES;
     if constexpr (JOIN) {
         h = blockIdx.y, b = blockIdx.z, split = blockIdx.x % A.splits, rb = blockIdx.x / A.splits;
+        if constexpr (TREE)
+            if (A.longest_first) b = of_rank(A.a.lens, A.a.B, b, lane);
     } else {
         h = blockIdx.x % A.c.heads;
         const int block = blockIdx.x / A.c.heads;
@@ -900,8 +914,8 @@ static fk_status launch_type(const AttendArgs& A, const KVPlan& p, hipStream_t s
 }
 
 template <bool TREE>
-static fk_status launch_attend(const KVView& c, const KVAttend& a, const KVPlan& p, hipStream_t s) {
-    const AttendArgs A{c, a, Divider(a.q_heads / c.heads), p.splits, p.row_blocks, (int)p.chunk, fmaxf(fabsf(a.scale) * 1.44269504088896341f, 1e-37f), a.scale < 0.f ? 0x80008000u : 0u};
+static fk_status launch_attend(const KVView& c, const KVAttend& a, const KVPlan& p, hipStream_t s, bool longest_first = false) {
+    const AttendArgs A{c, a, Divider(a.q_heads / c.heads), p.splits, p.row_blocks, (int)p.chunk, fmaxf(fabsf(a.scale) * 1.44269504088896341f, 1e-37f), a.scale < 0.f ? 0x80008000u : 0u, longest_first};
     return c.bf ? launch_type<true, TREE>(A, p, s) : launch_type<false, TREE>(A, p, s);
 }
 

@@ -15,8 +15,19 @@ namespace fk {
 // 34.3, one 50.9.
 static KVPlan choose_tree_plan(const KVView& c, int q_heads, int B, int max_q, int64_t reach) {
     KVPlan p = choose_kv_plan(c, q_heads, B, max_q, reach);
-    if (!p.join || p.splits > 1) return p;
     const int64_t rows = (int64_t)max_q * (q_heads / c.heads), ND = c.d / 32, units = device_cu_count(), steps = cdiv(reach, (int64_t)kJoinWaves * kStep);
+    if (!p.join && p.tiles > 1 && p.tiles == join_tiles((int)ND)) {
+        // Waves with rows of their own want two to a SIMD.  Trees often have fewer: then workgroups that share their rows are done sooner.  Both in tenths of a
+        // microsecond: a wave's step of 32 tokens takes 11 w / 10 alone on its SIMD and 6 w / 10 as one of several; a workgroup's of 256 tokens 16 w / 10, and
+        // rounds of them a time of their own.  16 trees of 60 tokens over 8000, 8 heads of 128, 4 queries each: 330 us with rows of their own,
+        // 220 shared; 32 of 30, 8 heads of 64, over 6000: 197 and 97; of 200 over 3000, enough waves, 244 with rows of their own.
+        const int64_t w = ND * p.tiles, waves = (int64_t)B * c.heads * cdiv(rows, 16 * p.tiles), each = cdiv(waves, 4 * units);
+        const int64_t own = 40 + cdiv(reach, (int64_t)kStep) * (each == 1 ? 11 * w : 6 * w * each) / 10;
+        const int64_t shared = cdiv(waves, units) * (80 + 5 * w + steps * 16 * w / 10);
+        if (shared < own) p.join = true;
+        return p;
+    }
+    if (!p.join || p.splits > 1) return p;
     int64_t least = INT64_MAX;
     for (int tiles = p.tiles; tiles >= 1; --tiles) {
         const int64_t blocks = (int64_t)B * c.heads * cdiv(rows, 16 * tiles), more = std::max(blocks - units, (int64_t)0), w = ND * tiles;
@@ -81,5 +92,9 @@ extern "C" fk_status fk_kv_attend_tree(const fk_kv_cache* cache, const void* q, 
     }
     const KVAttend a{{(const uint16_t*)q, q_token_stride, q_head_stride}, q_heads, Tq, pages, lens, q_start, max_pages, B, max_q,
                      scale, 0, window, (uint16_t*)out, lse, (float*)ws, tree, words};
-    return launch_attend<true>(c, a, p, (hipStream_t)stream);
+    const int64_t blocks = (int64_t)B * c.heads * p.row_blocks, steps = cdiv(reach_of(window, max_q + 1, max_len), (int64_t)kJoinWaves * kStep);
+    // Ragged sequences: the longest first, where there are rounds of workgroups and these are long enough for the look at the lengths.  8 trees of 121 tokens over
+    // up to 20000 361 us in the order of the call, 346 so; 40 of 64 over up to 4096 (16 steps) 126 and 133.
+    const bool longest_first = p.join && p.splits == 1 && !window && B > 1 && B <= 64 && blocks > device_cu_count() && steps >= 32;
+    return launch_attend<true>(c, a, p, (hipStream_t)stream, longest_first);
 }

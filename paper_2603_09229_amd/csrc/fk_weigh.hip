@@ -326,6 +326,8 @@ __global__ __launch_bounds__(kWeighThreads, !STREAM && ND <= 4 ? 4 : 2) void kv_
                     if (more) add_weights(0, Ss[1 - j], ls[1 - j], 0, false);
                     ls[1 - j] = l;
                 };
+                // (of a SIMD's two waves the older one is served first, and the other is what the block's barrier waits for: 508 us, so 501)
+                if (wave >= WAVES / 2) __builtin_amdgcn_s_setprio(1);
                 read_tile(place(0), Qs[0], ls[0]);
                 // (the last tile's logarithm is still wanted: ls[1] moves on only in the first body)
                 if (pending) {
@@ -338,6 +340,7 @@ __global__ __launch_bounds__(kWeighThreads, !STREAM && ND <= 4 ? 4 : 2) void kv_
                 interleave<0, ND>();
 #pragma unroll 1
                 for (int i = 2; i < each; i += 2) {
+                    if (2 * i >= each) __builtin_amdgcn_s_setprio(0);
                     body(i, std::integral_constant<int, 0>(), true);
                     interleave<0, ND>();
                     body(i + 1, std::integral_constant<int, 1>(), true);
