@@ -127,6 +127,19 @@ __global__ __launch_bounds__(kWeighThreads, !STREAM && ND <= 4 ? 4 : 2) void kv_
     const int nq = a.q_start ? min(min(max(a.q_start[b + 1] - q0, 0), a.max_q), (int)a.Tq - q0) : a.max_q;
     const int known = a.known ? a.known[b] : len, base = len - nq, rows = nq * A.group.by;
     const int step_tokens = TOKENS * token_waves;
+    if (!nq || (a.window && end - 1 <= base - a.window)) {         // no query sees any of these tokens
+        for (int t = begin + (int)threadIdx.x; t < end; t += THREADS) {
+            if (STREAM && A.splits > 1 && t < A.bound) {
+                a.part[((int64_t)unit * A.splits + split) * A.bound + t] = 0.f;
+                continue;
+            }
+            const int page = a.pages[(int64_t)b * a.max_pages + (t >> c.page_shift)];
+            if (split || page < 0 || page >= c.pages) continue;
+            const int64_t at = (((int64_t)page * c.heads + h) << c.page_shift) + (t & ((1 << c.page_shift) - 1));
+            a.out[at] = t < known ? a.decay * a.mass[at] : 0.f;
+        }
+        return;
+    }
 
     // A wave's tokens: page of token t0 + lane, codes, scales and weights so far, one step ahead.
     const int32_t* table = a.pages + (int64_t)b * a.max_pages;
