@@ -577,10 +577,22 @@ def fk_kv_weigh(cache: KVCache, q, lse, pages, lens, mass, *, q_start=None, max_
         status = L.fk_kv_weigh(*args, 0, 0, _raw_stream(cache))       # few queries need no workspace, and their calls are the short ones
         if status == _EWORKSPACE:
             room = max_pages * cache.page_size
-            ws = _workspace(cache, L.fk_kv_weigh_workspace_bytes(ref, heads, Tq, B, max_q, min(max_len or room, room)))
+            ws = _workspace(cache, fk_kv_weigh_workspace_bytes(cache, B, heads, Tq, max_q, min(max_len or room, room)))
             status = L.fk_kv_weigh(*args, ws.data_ptr(), ws.numel(), _raw_stream(cache))
         _check(status)
     return mass if out is None else out
+
+
+def fk_kv_weigh_workspace_bytes(cache: KVCache, B: int, q_heads: int, Tq: int, max_q: int, max_len: int) -> int:
+    """Bytes of `ws` for fk_kv_weigh of these sizes, and of these alone; 0 where it needs none.  max_len: at most what the page table has room for."""
+    _int32(B=B, q_heads=q_heads, max_q=max_q)
+    return int(lib().fk_kv_weigh_workspace_bytes(cache._here(), q_heads, Tq, B, max_q, max_len))
+
+
+def fk_kv_choose_workspace_bytes(cache: KVCache, B: int, max_len: int) -> int:
+    """Bytes of `ws` for fk_kv_choose; 0 where it needs none.  max_len: at most what the page table has room for."""
+    _int32(B=B)
+    return int(lib().fk_kv_choose_workspace_bytes(cache._here(), B, max_len))
 
 
 def fk_kv_choose(cache: KVCache, mass, pages, lens, keep: int, *, first: int = 0, last: int = 0, max_len: int = 0, kept=None, counts=None,
@@ -604,7 +616,7 @@ def fk_kv_choose(cache: KVCache, mass, pages, lens, keep: int, *, first: int = 0
         status = L.fk_kv_choose(*args, 0, 0, _raw_stream(cache))      # (as in fk_kv_weigh)
         if status == _EWORKSPACE:
             room = max_pages * cache.page_size
-            ws = _workspace(cache, L.fk_kv_choose_workspace_bytes(ref, B, min(max_len or room, room)))
+            ws = _workspace(cache, fk_kv_choose_workspace_bytes(cache, B, min(max_len or room, room)))
             status = L.fk_kv_choose(*args, ws.data_ptr(), ws.numel(), _raw_stream(cache))
         _check(status)
     return kept, counts

@@ -127,14 +127,13 @@ __global__ __launch_bounds__(kWeighThreads, !STREAM && ND <= 4 ? 4 : 2) void kv_
     const int nq = a.q_start ? min(min(max(a.q_start[b + 1] - q0, 0), a.max_q), (int)a.Tq - q0) : a.max_q;
     const int known = a.known ? a.known[b] : len, base = len - nq, rows = nq * A.group.by;
     const int step_tokens = TOKENS * token_waves;
-    if (!nq || (a.window && end - 1 <= base - a.window)) {         // no query sees any of these tokens
+    // Where no query sees any of these tokens, old weights are all there is.  (Where queries stream by, an exit of its own costs scalar registers, and the
+    // loops 2.5 %: the steps are gone through without keys and rows.)
+    const bool unseen = !nq || (a.window && end - 1 <= base - a.window), idle = STREAM && unseen;
+    if (!STREAM && unseen) {
         for (int t = begin + (int)threadIdx.x; t < end; t += THREADS) {
-            if (STREAM && A.splits > 1 && t < A.bound) {
-                a.part[((int64_t)unit * A.splits + split) * A.bound + t] = 0.f;
-                continue;
-            }
             const int page = a.pages[(int64_t)b * a.max_pages + (t >> c.page_shift)];
-            if (split || page < 0 || page >= c.pages) continue;
+            if (page < 0 || page >= c.pages) continue;
             const int64_t at = (((int64_t)page * c.heads + h) << c.page_shift) + (t & ((1 << c.page_shift) - 1));
             a.out[at] = t < known ? a.decay * a.mass[at] : 0.f;
         }
@@ -147,13 +146,16 @@ __global__ __launch_bounds__(kWeighThreads, !STREAM && ND <= 4 ? 4 : 2) void kv_
     int page;
     bool inside;                                                  // whether that page is one of the cache's: otherwise nothing is written
     uint32_t codes[PARTS][ND];
-    uint16_t scale;
+    uint16_t scale = 0;
     float old;
     int64_t at;                                                   // the cache's row of token t0 + lane
     auto ask_page = [&](int t0) { page = table[min(t0 + lane, last) >> c.page_shift]; };
     auto ask = [&](int t0) {
         inside = page >= 0 && page < c.pages;
         page = min(max(page, 0), (int)c.pages - 1);
+        at = (((int64_t)page * c.heads + h) << c.page_shift) + (min(t0 + lane, last) & ((1 << c.page_shift) - 1));
+        old = inside && t0 + lane < min(known, end) ? a.mass[at] : 0.f;
+        if (idle) return;
 #pragma unroll
         for (int u = 0; u < PARTS; ++u) {
             const int p = __builtin_amdgcn_readlane(page, 16 * u), first = min(t0 + 16 * u, last - 15) & ((1 << c.page_shift) - 1);
@@ -161,9 +163,7 @@ __global__ __launch_bounds__(kWeighThreads, !STREAM && ND <= 4 ? 4 : 2) void kv_
 #pragma unroll
             for (int k = 0; k < ND; ++k) codes[u][k] = load_at<uint32_t>(base, n * (16 * ND) + q * (4 * ND) + 4 * k);
         }
-        at = (((int64_t)page * c.heads + h) << c.page_shift) + (min(t0 + lane, last) & ((1 << c.page_shift) - 1));
         scale = c.k_scale[at];
-        old = inside && t0 + lane < min(known, end) ? a.mass[at] : 0.f;
     };
     ask_page(begin + token_wave * TOKENS);
 
@@ -240,7 +240,7 @@ __global__ __launch_bounds__(kWeighThreads, !STREAM && ND <= 4 ? 4 : 2) void kv_
             put_rows(1);
         }
     }
-    L::template fill<THREADS>(lds, level);
+    if (!idle) L::template fill<THREADS>(lds, level);
     ask(begin + token_wave * TOKENS);
     if (!STREAM) __syncthreads();
     const uint32_t copy = (lane & 31) * 4;
@@ -381,12 +381,14 @@ __global__ __launch_bounds__(kWeighThreads, !STREAM && ND <= 4 ? 4 : 2) void kv_
                 r_lo = (int)min((int64_t)r_lo + (int64_t)split * each, (int64_t)r_hi);
                 r_hi = (int)min((int64_t)r_lo + each, (int64_t)r_hi);
             }
-            place_rows(r_lo);
-            ask_rows(r_lo, r_hi);
+            if (!idle) {
+                place_rows(r_lo);
+                ask_rows(r_lo, r_hi);
+            }
             __syncthreads();                                      // (the table is there, the last step's rows are done with)
-            decode(0);
+            if (!idle) decode(0);
             if (more) ask(t0 + step_tokens);
-            put_rows(0);
+            if (!idle) put_rows(0);
             for (int r0 = r_lo, buffer = 0; r0 < r_hi; r0 += A.block_rows, buffer ^= 1) {
                 const int r1 = min(r0 + A.block_rows, r_hi);
                 __syncthreads();

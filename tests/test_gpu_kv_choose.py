@@ -110,7 +110,7 @@ def test_a_graph_and_a_used_workspace():
     cache, mass, table = make([30000, 500], 2, 64, 4, "weights")
     m, tb, lens = mass.to(DEV), table.to(DEV), torch.tensor([30000, 500], dtype=torch.int32, device=DEV)
     first = [x.clone() for x in fk.fk_kv_choose(cache, m, tb, lens, 300, first=4, last=20, max_len=30000)]
-    n = fk.lib().fk_kv_choose_workspace_bytes(cache._here(), 2, 30000)
+    n = fk.fk_kv_choose_workspace_bytes(cache, 2, 30000)
     ws = torch.full((n + 4096,), 91, dtype=torch.uint8, device=DEV)
     kept, counts = torch.empty_like(first[0]), torch.empty_like(first[1])
     call = lambda: fk.fk_kv_choose(cache, m, tb, lens, 300, first=4, last=20, max_len=30000, kept=kept, counts=counts, ws=ws[:n])  # noqa: E731

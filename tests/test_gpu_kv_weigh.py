@@ -186,3 +186,16 @@ def test_the_same_bits_every_time_and_under_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, first) and torch.equal(call(torch.zeros_like(start)), first)
+
+
+def test_rows_divided_among_workgroups_in_a_used_workspace():
+    """Few tokens and many queries: the parts' sums go through the workspace, whatever it holds, and nothing behind it is written."""
+    cache, q, lse, table, lens = small(15, 900, 1000)
+    n = fk.fk_kv_weigh_workspace_bytes(cache, 1, 2, 900, 900, 1000)
+    assert n > 0
+    first = fk.fk_kv_weigh(cache, q, lse, table, lens, torch.zeros(cache.pages, 1, 16, device=DEV), max_q=900, max_len=1000)
+    for fill in (0, 255, 127):
+        ws = torch.full((n + 4096,), fill, dtype=torch.uint8, device=DEV)
+        ws[n:] = 91
+        out = fk.fk_kv_weigh(cache, q, lse, table, lens, torch.zeros(cache.pages, 1, 16, device=DEV), max_q=900, max_len=1000, ws=ws[:n])
+        assert torch.equal(out, first) and (ws[n:] == 91).all()

@@ -128,3 +128,23 @@ def test_the_binding_refuses_integers_beyond_32_bits_before_it_looks_at_tensors(
             fk.fk_kv_weigh(Cache(), q, None, z, z[:, 0], None, **bad)
         with pytest.raises(ValueError):
             fk.fk_kv_attend_tree(Cache(), q, z, z[:, 0], torch.zeros(1, 1, dtype=torch.int64), **bad)
+
+
+def test_workspaces():
+    L, c = fk.lib(), ctypes.byref(cache(k_codes=None, k_levels=None))
+    weigh_bytes = lambda heads=32, Tq=1, B=1, max_q=1, max_len=1000: L.fk_kv_weigh_workspace_bytes(c, heads, Tq, B, max_q, max_len)  # noqa: E731
+    assert weigh_bytes() == 0 and weigh_bytes(max_len=1 << 30) == 0                     # few rows are not divided
+    assert weigh_bytes(max_q=2000, Tq=2000) > 0
+    for bad in (dict(heads=12), dict(max_len=0), dict(B=0), dict(max_q=0), dict(max_len=1 << 31)):
+        assert weigh_bytes(**bad) == 0 and L.fk_last_error()
+    choose_bytes = lambda B, max_len: L.fk_kv_choose_workspace_bytes(c, B, max_len)     # noqa: E731
+    assert choose_bytes(1, 16384) == 0 and choose_bytes(1, 16385) > 0 and choose_bytes(4096, 1 << 20) == 0
+    for bad in ((0, 100), (70000, 100), (1, 0), (1, 1 << 31)):
+        assert choose_bytes(*bad) == 0 and L.fk_last_error()
+    for B in (1, 2, 7, 30, 63, 64, 65, 1000, 65535):
+        sizes = [choose_bytes(B, n) for n in (1, 16384, 16385, 33000, 66000, 200000, 1 << 20, 1 << 24, 1 << 30)]
+        assert all(a <= b and b % 256 == 0 for a, b in zip(sizes, sizes[1:])) and sizes[-1] < 1 << 26
+        for max_q in (1, 33, 500, 4096, 1 << 20):
+            for n in (1, 100, 5000, 1 << 20, 1 << 30):
+                size = weigh_bytes(Tq=min(B * max_q, 1 << 30), B=B, max_q=max_q, max_len=n)
+                assert size % 256 == 0 and size < 1 << 26             # at most 64 parts of what fills the chip four times
