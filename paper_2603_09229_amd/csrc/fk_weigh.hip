@@ -13,7 +13,7 @@
 // Two forms.  Few rows (up to 128 at 128 channels) stay in LDS, and waves go over the tokens with the next step's codes on their way; the
 // workgroup's four waves a SIMD hide the rest.  Bound by bytes: 64 sequences of up to 8192 tokens, 8 heads of 128, 198 MB in 51 us, 3.9 TB/s
 // (one of 700: 4.4 us).  More rows stream by in blocks of two buffers, rows that all see all tokens with the products of a tile under
-// the exponentials of the one before it: 2 x 4096 queries of 32 heads over up to 9000 tokens, 426 GFLOP in 514 us, 0.83 PFLOP/s.
+// the exponentials of the one before it: 2 x 4096 queries of 32 heads over up to 9000 tokens, 426 GFLOP in 503 us, 0.85 PFLOP/s.
 // A tile of 16 rows and 64 tokens at d = 128 is 16 MFMA (256 cycles) and 16 times multiply-add, exponential and addition (another 256); alone
 // in a loop the two overlap to 412, here they take about 530: the rest is what a wave needs between tiles and at the blocks' barriers.
 // (Queries straight from memory, one launch of columns as rows: 1019 us and 151 for the batch.  Keys of 32 tokens and four waves a SIMD spill:
@@ -118,7 +118,7 @@ __global__ __launch_bounds__(kWeighThreads, !STREAM && ND <= 4 ? 4 : 2) void kv_
     const int units = c.heads * a.B, unit = blockIdx.x % units, split = blockIdx.x / units % A.splits, block = blockIdx.x / units / A.splits;
     const int h = unit % c.heads, b = unit / c.heads;
     const uint16_t level = c.k_levels[h * 16 + n];
-    const int token_waves = WAVES / A.row_waves, token_wave = wave & (token_waves - 1), row_wave = wave / token_waves;
+    const int row_waves = STREAM ? 1 : A.row_waves, token_waves = WAVES / row_waves, token_wave = wave & (token_waves - 1), row_wave = wave / token_waves;
     const int len = min(max(a.lens[b], 0), a.max_pages << c.page_shift);
     const int64_t begin64 = block * A.chunk;
     if (begin64 >= len) return;                                   // the whole workgroup
@@ -327,9 +327,8 @@ __global__ __launch_bounds__(kWeighThreads, !STREAM && ND <= 4 ? 4 : 2) void kv_
             const int p0 = base + A.group.quotient(r0), p1 = base + A.group.quotient(r1 - 1), first = t0 + 16 * u0, final = first + 16 * HOLD - 1;
             if ((a.causal && p1 < first) || (a.window && final <= p0 - a.window)) return;   // no row sees any of these tokens
             const bool masked = (a.causal && p0 < final) || (a.window && first <= p1 - a.window);
-            if (STREAM && !masked && count == TILES && TILES % (2 * A.row_waves) == 0) {
-                const int each = TILES / A.row_waves;
-                auto place = [&](int i) { return tile + row_wave + min(i, each - 1) * A.row_waves; };
+            if (STREAM && !masked && count == TILES) {
+                auto place = [&](int i) { return tile + min(i, TILES - 1); };
                 auto body = [&](int i, auto parity, bool more) {
                     constexpr int j = decltype(parity)::value;
                     floatx4 l;
@@ -352,8 +351,8 @@ __global__ __launch_bounds__(kWeighThreads, !STREAM && ND <= 4 ? 4 : 2) void kv_
                 body(1, std::integral_constant<int, 1>(), true);
                 interleave<0, ND>();
 #pragma unroll 1
-                for (int i = 2; i < each; i += 2) {
-                    if (2 * i >= each) __builtin_amdgcn_s_setprio(0);
+                for (int i = 2; i < TILES; i += 2) {
+                    if (2 * i >= TILES) __builtin_amdgcn_s_setprio(0);
                     body(i, std::integral_constant<int, 0>(), true);
                     interleave<0, ND>();
                     body(i + 1, std::integral_constant<int, 1>(), true);
@@ -365,10 +364,10 @@ __global__ __launch_bounds__(kWeighThreads, !STREAM && ND <= 4 ? 4 : 2) void kv_
             if (STREAM) flush();
             if (masked) {
 #pragma unroll 1
-                for (int i = row_wave; i < count; i += A.row_waves) add_tile(tile + i, u0, true);
+                for (int i = row_wave; i < count; i += row_waves) add_tile(tile + i, u0, true);
             } else {
 #pragma unroll 1
-                for (int i = row_wave; i < count; i += A.row_waves) add_tile(tile + i, u0, false);
+                for (int i = row_wave; i < count; i += row_waves) add_tile(tile + i, u0, false);
             }
         };
         if constexpr (STREAM) {
@@ -409,12 +408,12 @@ __global__ __launch_bounds__(kWeighThreads, !STREAM && ND <= 4 ? 4 : 2) void kv_
             }
         }
         float sum = add_rows(acc[0], acc[1], acc[2], acc[3]);     // of token t0 + lane
-        if (A.row_waves > 1) {
+        if (row_waves > 1) {
             __syncthreads();
             parts[wave][lane] = sum;
             __syncthreads();
             if (row_wave == 0)
-                for (int w = 1; w < A.row_waves; ++w) sum += parts[w * token_waves + token_wave][lane];
+                for (int w = 1; w < row_waves; ++w) sum += parts[w * token_waves + token_wave][lane];
         }
         if (row_wave || lane >= TOKENS || t0 + lane >= end) continue;
         if (divided) A.a.part[((int64_t)unit * A.splits + split) * A.bound + t0 + lane] = sum;
@@ -447,9 +446,13 @@ KVWeighPlan choose_weigh_plan(const KVView& c, int q_heads, int B, int max_q, in
     p.stream = rows > 2 * block_rows(ND, false);
     p.row_waves = p.splits = 1;
     const int tokens = weigh_tokens(ND, p.stream), most = std::min(kWeighWaves / 2, block_rows(ND, p.stream) / 16);
+    // Waves share their tokens and divide the rows where tokens alone do not fill the chip.  8 heads of 128, 32 queries of 4 heads, one sequence of 1000
+    // tokens: each its own 10.3 us, two share 7.8, four 6.5; of 20000: 13.4 and 18.4.
     while (!p.stream && 2 * p.row_waves <= most && tiles >= 4 * p.row_waves && cdiv(max_len, tokens * kWeighWaves / p.row_waves) * B * c.heads < units)
         p.row_waves *= 2;
     const int64_t step = tokens * kWeighWaves / p.row_waves, steps = cdiv(max_len, step), all = steps * B * c.heads;
+    // Steps of a workgroup: up to four, as long as there are four workgroups to a compute unit.  64 sequences of up to 8192: one 62 us, two 54, four 51, eight 54;
+    // 6 x 32 queries over up to 15000: one 18, two 22, four 29.
     p.chunk = (p.stream ? 1 : std::min((int64_t)4, std::max((int64_t)1, all / (4 * units)))) * step;
     p.blocks = (int)cdiv(max_len, p.chunk);
     if (p.stream) {
