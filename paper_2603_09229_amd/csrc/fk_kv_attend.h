@@ -524,8 +524,10 @@ struct Softmax {
 // JOIN: the waves of a workgroup share the rows and divide the tokens, each takes every kJoinWaves-th step (and workgroups may divide them
 // further); otherwise each wave has rows of its own, of one sequence or, where that has fewer tiles than a workgroup has waves, of
 // several, and takes all steps that they see.  Codes go straight from the cache into operands.
+// Two tiles of trees of 64 channels are held to 128 registers, so that workgroups run in pairs on a compute unit: 12 trees of 100 tokens over 5000
+// 124 us, where three tiles take 137 and four 132.
 template <bool BF, int ND, int NT, bool JOIN, bool TREE>
-__global__ __launch_bounds__(64 * (JOIN ? kJoinWaves : own_waves(NT)), NT == 1 && ND <= 4 ? 4 : JOIN ? 1 : 2)
+__global__ __launch_bounds__(64 * (JOIN ? kJoinWaves : own_waves(NT)), NT == 1 && ND <= 4 ? 4 : JOIN ? (TREE && NT == 2 && ND == 2 ? 4 : 1) : 2)
 void kv_attend_kernel(AttendArgs A) {
     // (a fixed size, so that the compiler knows the table's address and leaves it to the instruction's offset)
     using T = Table;

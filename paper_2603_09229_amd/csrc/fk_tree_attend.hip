@@ -10,9 +10,10 @@ namespace fk {
 
 // As for queries in a row, but for the tiles of workgroups that share their rows and do not divide the tokens.  A tree has some dozen query
 // tokens, more rows than one tile, and few sequences leave most of the chip idle: fewer tiles, and more workgroups that each decode the same codes.
-// The cost is the one that choose_kv_plan compares (tenths of a microsecond, steps of 256 tokens).  One tree of 13 tokens, 8 heads of 128,
-// 4 queries each, 700 tokens: three tiles 18.4 us, two 14.6, one 11.6; 8 of 60 over 1500: 53.6, 45.3, 47.1; 10 of 32, 4 heads of 160, 3000 tokens: two
-// 34.3, one 50.9.
+// The cost, in tenths of a microsecond, is fitted to 21 sizes from 32 to 256 channels, 9 to 100 tokens a tree and 300 to 6000 before it, 1 to 4 tiles: a
+// workgroup's first six steps of 256 tokens wait for memory more than later ones; those that hold at most 128 registers run in pairs on
+// a compute unit, others in rounds.  One tree of 13 tokens, 8 heads of 128, 4 queries each, 700 tokens: three tiles 18.2 us, two 14.4, one 11.3; 8 of
+// 60 over 1500: 53.5, 45.1, 47.4; 8 of 40, 8 heads of 64, over 6000: 43.1, 55.1, 58.6.
 static KVPlan choose_tree_plan(const KVView& c, int q_heads, int B, int max_q, int64_t reach) {
     KVPlan p = choose_kv_plan(c, q_heads, B, max_q, reach);
     const int64_t rows = (int64_t)max_q * (q_heads / c.heads), ND = c.d / 32, units = device_cu_count(), steps = cdiv(reach, (int64_t)kJoinWaves * kStep);
@@ -30,9 +31,14 @@ static KVPlan choose_tree_plan(const KVView& c, int q_heads, int B, int max_q, i
     if (!p.join || p.splits > 1) return p;
     int64_t least = INT64_MAX;
     for (int tiles = p.tiles; tiles >= 1; --tiles) {
-        const int64_t blocks = (int64_t)B * c.heads * cdiv(rows, 16 * tiles), more = std::max(blocks - units, (int64_t)0), w = ND * tiles;
-        const int64_t cost = w <= 2 || (tiles == 1 && ND <= 4) ? (40 + 5 * w + (4 + 3 * w) * steps) * units + (15 + w + (7 + 2 * w) * steps) * more
-                                                                : (60 + 2 * w + (10 + 2 * w) * steps) * cdiv(blocks, units) * units;
+        const int64_t blocks = (int64_t)B * c.heads * cdiv(rows, 16 * tiles), w = ND * tiles, early = std::min(steps, (int64_t)6), late = steps - early;
+        int64_t cost = 0;
+        if (w <= 2 || (tiles == 1 && ND <= 4) || (tiles == 2 && ND == 2)) {
+            const int64_t more = std::max(blocks - units, (int64_t)0);
+            cost = 50 + 6 * w + 16 * early + (6 + w) * late + (17 * w + (46 + 8 * w) * steps / 10) * (more + cdiv(more, units) * units) / (2 * units);
+        } else {
+            cost = (140 + 11 * w - 24 * (6 - early) + (35 + 12 * w) * late / 10) * cdiv(blocks, units);
+        }
         if (cost < least) {
             least = cost;
             p.tiles = tiles;
