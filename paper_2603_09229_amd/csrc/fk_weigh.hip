@@ -13,9 +13,9 @@
 // Two forms.  Few rows (up to 128 at 128 channels) stay in LDS, and waves go over the tokens with the next step's codes on their way; the
 // workgroup's four waves a SIMD hide the rest.  Bound by bytes: 64 sequences of up to 8192 tokens, 8 heads of 128, 198 MB in 51 us, 3.9 TB/s
 // (one of 700: 4.4 us).  More rows stream by in blocks of two buffers, rows that all see all tokens with the products of a tile under
-// the exponentials of the one before it: 2 x 4096 queries of 32 heads over up to 9000 tokens, 426 GFLOP in 503 us, 0.85 PFLOP/s.
+// the exponentials of the one before it: 2 x 4096 queries of 32 heads over up to 9000 tokens, 426 GFLOP in 482 us, 0.88 PFLOP/s.
 // A tile of 16 rows and 64 tokens at d = 128 is 16 MFMA (256 cycles) and 16 times multiply-add, exponential and addition (another 256); alone
-// in a loop the two overlap to 412, here they take about 530: the rest is what a wave needs between tiles and at the blocks' barriers.
+// in a loop the two overlap to 412, here they take about 500: the rest is what a wave needs between tiles and at the blocks' barriers.
 // (Queries straight from memory, one launch of columns as rows: 1019 us and 151 for the batch.  Keys of 32 tokens and four waves a SIMD spill:
 // 1054.  16-byte pieces gathered in the lanes' order instead of whole rows: 774 against 609 at that step.)
 #include <algorithm>
@@ -49,7 +49,8 @@ struct WeighArgs {
 
 // LDS: the table of pairs of the keys' levels, 256 rows of 32 copies, in the lower halves of rows of 256 bytes (a byte of codes is then the
 // address with one v_perm), and the queries in the upper ones, in the order in which a wave's lanes read them as operands, 16 bytes a lane.
-// Lanes that write a row's pieces meet in a bank unless the rows' order within a piece's slot is turned by the piece.
+// Lanes that write a row's pieces meet in a bank unless the rows' order within a piece's slot is turned by the piece, and by no more of the quarter
+// than its upper bit, or lanes of two quarters meet when they read (conflicts 39 % of the LDS's time, so 13 %).
 template <bool STREAM>
 struct WeighLds {
     static constexpr int bytes = 65536 * (STREAM ? 2 : 1), piece_bytes = STREAM ? 1024 : 2048;
@@ -57,7 +58,7 @@ struct WeighLds {
     // piece k of quarter q of row n of a tile
     template <int ND>
     static __device__ __forceinline__ int piece(int tile, int k, int q, int n) {
-        return slot_byte((tile * ND + k) * 64 + q * 16 + (n ^ (((q * 4) ^ k) & 15)));
+        return slot_byte((tile * ND + k) * 64 + q * 16 + (n ^ ((q >> 1) * 8) ^ k));
     }
     template <int THREADS>
     static __device__ __forceinline__ void fill(uint8_t* lds, uint16_t level) {
@@ -73,7 +74,6 @@ struct WeighLds {
 // the upper halves of the first and the lower halves of the second register change places, in units of BY lanes
 template <int BY>
 __device__ __forceinline__ void swap_lanes(float& a, float& b) {
-    typedef uint32_t uintx2v __attribute__((ext_vector_type(2)));
     const auto r = BY == 32 ? __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false)
                             : __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
     a = __uint_as_float(r[0]);
