@@ -776,7 +776,7 @@ void kv_attend_kernel(AttendArgs A) {
 // the splits' factors in LDS; then each of the waves adds its share of the splits' products, and the first wave what they have.  Few
 // splits (many sequences) take one wave, many eight.  What the workspace holds is read before it is known which splits have written
 // anything; the others are left out afterwards, whatever their places hold.
-template <bool BF, int ND, int NT, int WAVES, int MOST>
+template <bool BF, int ND, int NT, int WAVES, int MOST, bool TREE>
 __global__ __launch_bounds__(64 * WAVES, 4) void kv_join_kernel(AttendArgs A) {
     constexpr int R = 16 * NT, LANES = 4 * WAVES, EACH = MOST / LANES, EARLY = 4;
     __shared__ floatx4 swap[WAVES][64];
@@ -806,7 +806,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void kv_join_kernel(AttendArgs A) {
     if (row0 + c * 16 >= rows) return;
     const int i0 = A.group.quotient(row0), i1 = A.group.quotient(min(row0 + R, rows) - 1);
     const int hi = a.causal ? max(min(len, len - nq + i1 + 1), 0) : len;
-    const int lo = (a.window ? max(0, len - nq + (a.tree ? -1 : i0) - a.window + 1) : 0) & ~(kStep - 1);
+    const int lo = (a.window ? max(0, len - nq + (TREE ? -1 : i0) - a.window + 1) : 0) & ~(kStep - 1);
     if (hi - lo <= A.chunk) return;                               // one split has written the result itself
     const int parts = min(A.splits, (hi - lo + A.chunk - 1) / A.chunk);
 
@@ -871,8 +871,8 @@ static fk_status launch_form(const AttendArgs& A, hipStream_t s) {
     FK_HIP(hipGetLastError());
     if (A.splits > 1) {
         const dim3 grid(A.row_blocks * 2 * ND * NT, A.c.heads, A.a.B);
-        if (A.splits <= 8) kv_join_kernel<BF, ND, NT, 1, 8><<<grid, 64, 0, s>>>(A);
-        else kv_join_kernel<BF, ND, NT, 8, kMostSplits><<<grid, 512, 0, s>>>(A);
+        if (A.splits <= 8) kv_join_kernel<BF, ND, NT, 1, 8, TREE><<<grid, 64, 0, s>>>(A);
+        else kv_join_kernel<BF, ND, NT, 8, kMostSplits, TREE><<<grid, 512, 0, s>>>(A);
         FK_HIP(hipGetLastError());
     }
     return FK_OK;

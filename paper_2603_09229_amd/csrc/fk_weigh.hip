@@ -16,7 +16,7 @@
 // the exponentials of the one before it: 2 x 4096 queries of 32 heads over up to 9000 tokens, 426 GFLOP in 482 us, 0.88 PFLOP/s.
 // A tile of 16 rows and 64 tokens at d = 128 is 16 MFMA (256 cycles) and 16 times multiply-add, exponential and addition (another 256); alone
 // in a loop the two overlap to 412, here they take about 500: the rest is what a wave needs between tiles and at the blocks' barriers.
-// (Queries straight from memory, one launch of columns as rows: 1019 us and 151 for the batch.  Keys of 32 tokens and four waves a SIMD spill:
+// (The simple form, tokens on the tiles' row side and each wave reading the queries from memory: 1019 us.  Keys of 32 tokens and four waves a SIMD spill:
 // 1054.  16-byte pieces gathered in the lanes' order instead of whole rows: 774 against 609 at that step.)
 #include <algorithm>
 #include <type_traits>
