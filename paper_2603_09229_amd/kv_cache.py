@@ -107,14 +107,15 @@ class Server:
         more than max_len tokens or pass position max_pos (they would have no page, or no angle)."""
         if len(counts) != len(self.lens) or any(c < 0 for c in counts) or not sum(counts) == len(q) == len(k) == len(v):
             raise ValueError(f"counts {counts} for {len(self.lens)} sequences and rows of {len(q)}, {len(k)}, {len(v)} tokens")
-        held = self.lens.tolist()
+        limited = self.max_pos is not None
+        held, *gone = torch.stack((self.lens, self.gone)).tolist() if limited else [self.lens.tolist()]
         over = [b for b, (h, c) in enumerate(zip(held, counts)) if h + c > self.max_len]
         if over:
             raise ValueError(f"sequences {over} would hold more than {self.max_len} tokens")
         if self._draft is not None:
             raise ValueError("drafted tokens wait for accept()")
-        if self.max_pos is not None and self.max_pos > self.max_len:
-            over = [b for b, (h, g, c) in enumerate(zip(held, self.gone.tolist(), counts)) if h + g + c > self.max_pos]
+        if limited:
+            over = [b for b, (h, g, c) in enumerate(zip(held, *gone, counts)) if h + g + c > self.max_pos]
             if over:
                 raise ValueError(f"sequences {over} would pass position {self.max_pos}")
 
