@@ -102,9 +102,10 @@ class Server:
         if weights:
             self.mass = torch.zeros(self.cache.k_scale.shape, dtype=torch.float32, device=dev)
 
-    def _check(self, q, k, v, counts: list[int]):
+    def _check(self, q, k, v, counts: list[int], levels: list[int] | None = None):
         """Refused before anything changes: counts that are not one for each sequence or not those of the rows, and a sequence that would hold
-        more than max_len tokens or pass position max_pos (they would have no page, or no angle)."""
+        more than max_len tokens or pass position max_pos (they would have no page, or no angle).  levels: how many positions a sequence's
+        tokens take, where that is not one each."""
         if len(counts) != len(self.lens) or any(c < 0 for c in counts) or not sum(counts) == len(q) == len(k) == len(v):
             raise ValueError(f"counts {counts} for {len(self.lens)} sequences and rows of {len(q)}, {len(k)}, {len(v)} tokens")
         limited = self.max_pos is not None
@@ -115,7 +116,7 @@ class Server:
         if self._draft is not None:
             raise ValueError("drafted tokens wait for accept()")
         if limited:
-            over = [b for b, (h, g, c) in enumerate(zip(held, *gone, counts)) if h + g + c > self.max_pos]
+            over = [b for b, (h, g, c) in enumerate(zip(held, *gone, levels or counts)) if h + g + c > self.max_pos]
             if over:
                 raise ValueError(f"sequences {over} would pass position {self.max_pos}")
 
@@ -158,8 +159,9 @@ class Server:
         """A tree of drafted tokens for each sequence (parents as in tree_masks, rows as in `step`, trees may be empty) -> attention of each
         token over what the sequence holds and its branch [T, q_heads, d].  `accept` says which of them stay."""
         counts = [len(tree) for tree in parents]
-        self._check(q, k, v, counts)
         masks, depths = tree_masks(parents, q.device)
+        left = iter(depths)
+        self._check(q, k, v, counts, [max((next(left) + 1 for _ in tree), default=0) for tree in parents])   # (tokens of a level share a position)
         if not sum(counts):
             return torch.empty_like(q)
         q, start = self._append(q, k, v, counts, depths)

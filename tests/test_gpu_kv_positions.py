@@ -6,6 +6,7 @@ import pytest
 import torch
 
 from paper_2603_09229_amd import kv_cache
+from tests import evict_plain as plain
 from tests import kv_plain
 from tests.test_gpu_kv_drafts import DEV, check, values
 
@@ -33,3 +34,24 @@ def test_a_server_without_max_pos_evicts_and_stops_at_its_last_angle(dtype):
             call()
     assert all(torch.equal(x, y) for x, y in zip(was, (server.cache.k_codes, server.mass, server.lens, server.gone)))
     assert server.step(*draw(1), [0, 1]).isfinite().all()         # the other one goes on
+
+
+def test_a_wide_tree_up_to_the_last_angle():
+    g = torch.Generator().manual_seed(12)
+    H, G, d = 2, 4, 64
+    server = kv_cache.Server(*[kv_plain.levels(H, torch.float16, s, DEV) for s in (7, 8)], d, 1, 80, page_size=16, max_pos=83, weights=True)
+    draw = lambda n: [torch.randn(n, h, d, generator=g).half().to(DEV) for h in (H * G, H, H)]  # noqa: E731
+    server.step(*draw(80), [80])
+    server.evict(50, 4, 10)
+    tree = [-1] * 10 + list(range(10)) + list(range(10, 20))      # 30 tokens, positions 80 to 82
+    q, k, v = draw(30)
+    out = server.draft(q, k, v, [tree])
+    masks, depths = kv_cache.tree_masks([tree])
+    assert max(depths) == 2
+    qt = kv_plain.turned(q, server.cos_sin, torch.tensor([80 + x for x in depths], device=DEV), False)
+    sees = [plain.tree_sees([m[0] for m in masks.tolist()], 80, 30, 0)]
+    want, _, mag, err = plain.attend(*values(server), qt, server.pages, [80], [0, 30], 1 / math.sqrt(d), sees)
+    check(out, want, mag, err, torch.float16)
+    server.accept([[3, 13, 23]])
+    with pytest.raises(ValueError, match="position 83"):
+        server.step(*draw(1), [1])

@@ -28,3 +28,22 @@ def test_the_last_position_is_given_out():
     s._check(*rows(5, 5, 5), [2, 3])                              # up to position 19 of 20
     with pytest.raises(ValueError, match=r"sequences \[0\] would pass position 20"):
         s._check(*rows(6, 6, 6), [3, 3])
+
+
+class Passed(Exception):
+    """What a server here does instead of its first launch."""
+
+
+def test_a_wide_tree_is_measured_by_its_depth():
+    """Drafted tokens stand side by side: 60 of them in 3 levels take 60 places, and 3 positions."""
+    def launch(*_):
+        raise Passed
+    tree = [-1] * 20 + list(range(40))
+    for gone, refused in (([97, 0], None), ([98, 0], 0), ([0, 97], None), ([0, 98], 1)):
+        s = evicted([0, 0], gone, max_len=60, max_pos=100)
+        s._append = launch
+        trees = [tree, [-1]] if gone[0] else [[-1], tree]
+        with pytest.raises(ValueError, match="more than 60 tokens"):
+            s.draft(*rows(62, 62, 62), [t + [0] if t is tree else t for t in trees])
+        with pytest.raises(Passed) if refused is None else pytest.raises(ValueError, match=rf"sequences \[{refused}\] would pass position 100"):
+            s.draft(*rows(61, 61, 61), trees)
