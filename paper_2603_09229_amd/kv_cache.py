@@ -83,6 +83,7 @@ class Server:
     max_pos = None
     mass = None                                                       # attention weights of the cached tokens, with `weights`
     _draft = None                                                     # the drafted trees that wait for `accept`
+    _empty = False                                                    # the last call was a draft without any: nothing waits
 
     def __init__(self, k_levels, v_levels, d: int, batch: int, max_len: int, page_size: int = 64, max_pos: int | None = None,
                  weights: bool = False):
@@ -119,6 +120,7 @@ class Server:
             over = [b for b, (h, g, c) in enumerate(zip(held, *gone, levels or counts)) if h + g + c > self.max_pos]
             if over:
                 raise ValueError(f"sequences {over} would pass position {self.max_pos}")
+        self._empty = False
 
     def _append(self, q, k, v, counts: list[int], depths: list[int] | None = None):
         """New rows into the cache behind what the sequences hold -> (turned queries, starts); lens is left as it is.  depths: the
@@ -163,6 +165,7 @@ class Server:
         left = iter(depths)
         self._check(q, k, v, counts, [max((next(left) + 1 for _ in tree), default=0) for tree in parents])   # (tokens of a level share a position)
         if not sum(counts):
+            self._empty = True
             return torch.empty_like(q)
         q, start = self._append(q, k, v, counts, depths)
         held = self.lens + torch.tensor(counts, dtype=torch.int32, device=q.device)
@@ -174,15 +177,15 @@ class Server:
 
     def accept(self, branches: list[list[int]]):
         """The drafted tokens that each sequence keeps, a branch from a root down, or none of them; the others are forgotten."""
-        if self._draft is None:
+        if self._draft is None and not self._empty:
             raise ValueError("there is no draft")
-        parents, q, lse = self._draft
+        parents, q, lse = self._draft or ([[]] * len(self.lens), None, None)
         if len(branches) != len(parents):
             raise ValueError(f"{len(branches)} branches for {len(parents)} sequences")
         for tree, branch in zip(parents, branches):
             if any(not 0 <= i < len(tree) or tree[i] != p for p, i in zip([-1] + branch, branch)):
                 raise ValueError(f"{branch} is no branch from a root of the tree {tree}")
-        self._draft = None
+        self._draft, self._empty = None, False
         counts, most = [len(branch) for branch in branches], max(map(len, branches))
         if not most:
             return
