@@ -172,7 +172,7 @@ class Server:
         out = fk.fk_kv_attend_tree(self.cache, q, self.pages, held, masks, q_start=start, max_q=max(counts), max_len=self.max_len,
                                    lse=self.mass is not None)
         out, lse = out if self.mass is not None else (out, None)
-        self._draft = (parents, q, lse)
+        self._draft = ([list(tree) for tree in parents], q, lse)
         return out
 
     def accept(self, branches: list[list[int]]):
