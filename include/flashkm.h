@@ -395,7 +395,8 @@ fk_status fk_kv_attend_tree(const fk_kv_cache* cache, const void* q, int64_t q_t
  *   group that see the token
  * for every place of [0, lens[b]) and every cache head; other places are left as they are.
  *   mass, mass_out   device, [pages, heads, page_size] float, as the cache's scales lie; they may be one tensor, otherwise they do not overlap.
- *   lse              device, [Tq, q_heads] float, as fk_kv_attend gives it for these queries; a row with -inf adds nothing
+ *   lse              device, [Tq, q_heads] float, as fk_kv_attend gives it for these queries; a row with -inf adds nothing, whatever its query
+ *                    holds (padded rows, say) and whatever the keys are that it alone would see
  *   known            device, [B] int32, or NULL: tokens from place known[b] on have no weights yet, and what mass holds of them is not
  *                    read.  lens[b] less the new tokens for a decoding step, 0 for a prompt; NULL: all have.
  *   decay            finite; 1 adds up, less than 1 lets older weights fade

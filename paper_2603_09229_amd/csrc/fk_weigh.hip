@@ -111,6 +111,8 @@ __global__ __launch_bounds__(kWeighThreads, !STREAM && ND <= 4 ? 4 : 2) void kv_
     __shared__ __align__(16) float logs[2 * HB];                  // of a row: its logarithm in powers of two,
     __shared__ __align__(16) int upto[2 * HB], from[2 * HB];      // and it sees the tokens behind `from` up to `upto`
     __shared__ float parts[WAVES][64];
+    constexpr int GROUPS = (HB + 63) / 64;                        // of 64 rows of a buffer: whether one of them
+    __shared__ int mute[2][GROUPS];                               // adds nothing, whatever its query and what it sees
     const KVWeigh& a = A.a;
     const KVView& c = A.c;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63, n = lane & 15, q = lane >> 4;
@@ -222,10 +224,14 @@ __global__ __launch_bounds__(kWeighThreads, !STREAM && ND <= 4 ? 4 : 2) void kv_
             if (row < HB) *(uintx4*)(lds + buffer * (TILES * ND * L::piece_bytes) + L::template piece<ND>(row / 16, p % ND, p / ND, row & 15)) = piece[e];
         }
         if (threadIdx.x < HB) {
-            // of a row that is none, or that has seen nothing: weights of 0
-            logs[buffer * HB + threadIdx.x] = log_in == -INFINITY ? INFINITY : log_in * 1.44269504088896341f;
-            upto[buffer * HB + threadIdx.x] = upto_in;
+            // Of a row that is none, or that has seen nothing: weights of 0.  The second sees nothing here either, and its tiles are masked: its query,
+            // or a key that it alone would see, need not be finite.
+            const bool none = log_in == -INFINITY;
+            logs[buffer * HB + threadIdx.x] = none ? INFINITY : log_in * 1.44269504088896341f;
+            upto[buffer * HB + threadIdx.x] = none ? -1 : upto_in;
             from[buffer * HB + threadIdx.x] = from_in;
+            const bool any = __any(none && upto_in >= 0);
+            if (lane == 0) mute[buffer][wave] = any;
         }
     };
     int tiles = 0;
@@ -243,6 +249,14 @@ __global__ __launch_bounds__(kWeighThreads, !STREAM && ND <= 4 ? 4 : 2) void kv_
     if (!idle) L::template fill<THREADS>(lds, level);
     ask(begin + token_wave * TOKENS);
     if (!STREAM) __syncthreads();
+    auto muted = [&](int buffer) {
+        int any = mute[buffer][0];
+#pragma unroll
+        for (int i = 1; i < GROUPS; ++i) any |= mute[buffer][i];
+        return any;
+    };
+    int hushed = 0;                                               // whether one of the rows that are kept, or of the block, is such a row
+    if (!STREAM && tiles) hushed = muted(0) | (rows > HB ? muted(1) : 0);
     const uint32_t copy = (lane & 31) * 4;
     const int q_lane = L::template piece<ND>(0, 0, q, n);           // (piece k: its bits 4 to 6 turned by k)
 
@@ -326,7 +340,7 @@ __global__ __launch_bounds__(kWeighThreads, !STREAM && ND <= 4 ? 4 : 2) void kv_
         auto add_tiles = [&](int tile, int count, int r0, int r1, int u0) {
             const int p0 = base + A.group.quotient(r0), p1 = base + A.group.quotient(r1 - 1), first = t0 + 16 * u0, final = first + 16 * HOLD - 1;
             if ((a.causal && p1 < first) || (a.window && final <= p0 - a.window)) return;   // no row sees any of these tokens
-            const bool masked = (a.causal && p0 < final) || (a.window && first <= p1 - a.window);
+            const bool masked = (a.causal && p0 < final) || (a.window && first <= p1 - a.window) || __builtin_amdgcn_readfirstlane(hushed);
             if (STREAM && !masked && count == TILES) {
                 auto place = [&](int i) { return tile + min(i, TILES - 1); };
                 auto body = [&](int i, auto parity, bool more) {
@@ -391,6 +405,7 @@ __global__ __launch_bounds__(kWeighThreads, !STREAM && ND <= 4 ? 4 : 2) void kv_
             for (int r0 = r_lo, buffer = 0; r0 < r_hi; r0 += A.block_rows, buffer ^= 1) {
                 const int r1 = min(r0 + A.block_rows, r_hi);
                 __syncthreads();
+                hushed = muted(buffer);
                 if (r1 < r_hi) {
                     if (!A.whole_tokens) place_rows(r1);
                     ask_rows(r1, r_hi);
