@@ -420,7 +420,7 @@ size_t fk_kv_weigh_workspace_bytes(const fk_kv_cache* cache, int q_heads, int64_
  *   pages, lens, max_len   as for fk_kv_attend
  *   keep     >= 1, first + last <= keep
  *   kept     device out, [B, heads, keep] int32: the places in ascending order, -1 behind them; all of a sequence of up to `keep` tokens
- *   counts   device out, [B] int32: min(lens, keep)
+ *   counts   device out, [B] int32: min(lens, keep); not in the place of lens
  *   ws       device, fk_kv_choose_workspace_bytes(...) bytes, 256-byte aligned, contents undefined before and after; NULL if that is 0
  *            (max_len >= 1, at most max_pages * page_size counts)
  */

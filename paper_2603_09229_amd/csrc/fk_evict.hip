@@ -98,6 +98,10 @@ fk_status fk_kv_choose(const fk_kv_cache* cache, const float* mass, const int32_
     FK_TRY(need(fn, "lens", lens, 4));
     FK_TRY(need(fn, "kept", kept, 4));
     FK_TRY(need(fn, "counts", counts, 4));
+    if (counts < lens + B && lens < counts + B) {                 // (workgroups of all heads read lens, one of them writes counts)
+        set_error("%s: counts overlaps lens", fn);
+        return FK_EINVAL;
+    }
     max_len = max_len ? std::min(max_len, room) : room;
     const size_t bytes = choose_workspace_bytes(c, B, max_len);
     if (ws_bytes < bytes) {
