@@ -130,12 +130,13 @@ class Server:
         start = torch.zeros(len(counts) + 1, dtype=torch.int32, device=dev)
         start[1:] = n.cumsum(0)
         seq = torch.repeat_interleave(torch.arange(len(counts), device=dev), n, output_size=len(q))
-        behind = torch.arange(len(q), device=dev, dtype=torch.int32) - start[seq]
-        place = self.lens[seq] + behind
+        place = self.lens[seq] + torch.arange(len(q), device=dev, dtype=torch.int32) - start[seq]
         slots = self.pages[seq, (place // P).long()].long() * P + place % P
+        positions = place
         if depths is not None:
-            behind = torch.tensor(depths, dtype=torch.int32, device=dev)
-        positions = self.lens[seq] + self.gone[seq] + behind
+            positions = (self.lens + self.gone)[seq] + torch.tensor(depths, dtype=torch.int32, device=dev)
+        elif self.mass is not None:                                   # (otherwise nothing is ever evicted)
+            positions = place + self.gone[seq]
         return fk.fk_kv_append(self.cache, k, v, slots, positions=positions, cos_sin=self.cos_sin, q=q), start
 
     def _weigh(self, q, lse, start, most: int, before):
@@ -148,7 +149,7 @@ class Server:
             return torch.empty_like(q)
         q, start = self._append(q, k, v, counts)
         before = self.lens.clone() if self.mass is not None else None
-        self.lens += torch.tensor(counts, dtype=torch.int32, device=q.device)
+        self.lens += start.diff()
         out = fk.fk_kv_attend(self.cache, q, self.pages, self.lens, q_start=start, max_q=max(counts), max_len=self.max_len,
                               lse=self.mass is not None)
         if self.mass is None:
@@ -168,7 +169,7 @@ class Server:
             self._empty = True
             return torch.empty_like(q)
         q, start = self._append(q, k, v, counts, depths)
-        held = self.lens + torch.tensor(counts, dtype=torch.int32, device=q.device)
+        held = self.lens + start.diff()
         out = fk.fk_kv_attend_tree(self.cache, q, self.pages, held, masks, q_start=start, max_q=max(counts), max_len=self.max_len,
                                    lse=self.mass is not None)
         out, lse = out if self.mass is not None else (out, None)
