@@ -381,13 +381,17 @@ int fk_kv_plan(const fk_kv_cache* cache, int q_heads, int B, int max_q, int64_t 
  *            mask will do: for the tree of a draft a row has the token itself and its ancestors.  Bits from n on are ignored.
  *   words    of a row; 64 * words >= max_q, Tq * words < 2^29
  *   window   > 0: of the tokens that a query would see, in the order of their places, only the last `window`; 0: no such limit
- * A row that sees nothing gives 0 and lse -inf.  The workspace is that of fk_kv_attend for these sizes.
+ * A row that sees nothing gives 0 and lse -inf.  The workspace is that of fk_kv_attend for these sizes, and so is the arithmetic: weights are rounded
+ * to fp16 for the product with the values.
  */
 fk_status fk_kv_attend_tree(const fk_kv_cache* cache, const void* q, int64_t q_token_stride, int64_t q_head_stride,
                             int q_heads, int64_t Tq, const int32_t* pages, int max_pages, const int32_t* lens,
                             const int32_t* q_start, int B, int max_q, int64_t max_len, float scale, int window,
                             const uint64_t* tree, int words, void* out, float* lse, void* ws, size_t ws_bytes,
                             void* stream);
+/* What fk_kv_attend_tree would launch for these sizes, in the words of fk_kv_plan; "longest_first": workgroups look at the lengths, and long
+ * sequences come first. */
+int fk_kv_plan_tree(const fk_kv_cache* cache, int q_heads, int B, int max_q, int64_t max_len, int window, char* buf, size_t buf_bytes);
 
 /*
  * Attention weights added up over queries, a number a token and cache head: what eviction goes by.

@@ -24,7 +24,7 @@ EXPORTS = ("fk_last_error", "fk_workspace_bytes", "fk_assign", "fk_sort_inverse"
            "fk_stage_timer_stop", "fk_plan", "fk_set_option", "fk_standard_assign",
            "fk_standard_update", "fk_assign_static", "fk_assign_static_limit", "fk_kv_append", "fk_kv_read",
            "fk_kv_attend", "fk_kv_workspace_bytes", "fk_kv_plan", "fk_kv_attend_tree", "fk_kv_weigh", "fk_kv_weigh_workspace_bytes", "fk_kv_choose",
-           "fk_kv_choose_workspace_bytes", "fk_kv_compact")
+           "fk_kv_choose_workspace_bytes", "fk_kv_compact", "fk_kv_plan_tree")
 STAGES = ("assign", "sort", "reduce", "finalize")
 
 
@@ -101,6 +101,8 @@ def lib() -> ctypes.CDLL:
         L.fk_kv_compact.argtypes = [cache, vp, i32, vp, i32, i32, vp, vp, vp, i32, i32, vp, vp]
         L.fk_kv_plan.restype = i32
         L.fk_kv_plan.argtypes = [cache, i32, i32, i32, i64, i32, ctypes.c_char_p, sz]
+        L.fk_kv_plan_tree.restype = i32
+        L.fk_kv_plan_tree.argtypes = L.fk_kv_plan.argtypes
         L.fk_plan.restype = i32
         L.fk_plan.argtypes = [i32, i64, i32, i32, i32, ctypes.c_char_p, sz]
         L.fk_set_option.restype = i32
@@ -472,14 +474,23 @@ def make_kv_workspace(cache: KVCache, B: int, q_heads: int, Tq: int, max_q: int,
     return torch.empty(n, dtype=torch.uint8, device=cache.device)
 
 
-def fk_kv_plan(cache: KVCache, B: int, q_heads: int, max_q: int, max_len: int, window: int = 0) -> str:
-    """One-line description of what fk_kv_attend would launch for these sizes."""
+def _plan(call, cache: KVCache, B: int, q_heads: int, max_q: int, max_len: int, window: int) -> str:
     _int32(B=B, q_heads=q_heads, max_q=max_q)
     buf = ctypes.create_string_buffer(256)
     window = min(window, 2 ** 31 - 1)                                 # as in fk_kv_attend
     _int32(window=window)
-    _check(lib().fk_kv_plan(cache._here(), q_heads, B, max_q, max_len, window, buf, len(buf)))
+    _check(call(cache._here(), q_heads, B, max_q, max_len, window, buf, len(buf)))
     return buf.value.decode()
+
+
+def fk_kv_plan(cache: KVCache, B: int, q_heads: int, max_q: int, max_len: int, window: int = 0) -> str:
+    """One-line description of what fk_kv_attend would launch for these sizes."""
+    return _plan(lib().fk_kv_plan, cache, B, q_heads, max_q, max_len, window)
+
+
+def fk_kv_plan_tree(cache: KVCache, B: int, q_heads: int, max_q: int, max_len: int, window: int = 0) -> str:
+    """One-line description of what fk_kv_attend_tree would launch for these sizes."""
+    return _plan(lib().fk_kv_plan_tree, cache, B, q_heads, max_q, max_len, window)
 
 
 _EWORKSPACE = 3

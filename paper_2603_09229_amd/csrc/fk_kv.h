@@ -87,6 +87,10 @@ bool view_of(const char* fn, const fk_kv_cache* c, bool pointers, KVView* v, fk_
 // A device pointer that has to be there, aligned to `to` bytes.
 fk_status need(const char* fn, const char* name, const void* p, size_t to);
 fk_status check_queries(const char* fn, const KVView& c, int q_heads, int64_t Tq, int B, int max_q, int64_t max_len);
+// Sizes of a plan that is asked for, with the text of one that there is none of; and a plan as text, with what a form adds to it.
+fk_status check_plan(const char* fn, const fk_kv_cache* cache, int q_heads, int B, int max_q, int64_t max_len, int window, char* buf, size_t buf_bytes,
+                     KVView* c);
+void describe_plan(const KVPlan& p, const KVView& c, int B, const char* more, char* buf, size_t buf_bytes);
 // The most tokens that the queries of a sequence see together.
 int64_t reach_of(int window, int max_q, int64_t max_len);
 

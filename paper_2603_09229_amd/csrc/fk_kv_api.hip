@@ -73,6 +73,33 @@ int64_t reach_of(int window, int max_q, int64_t max_len) {
     return window ? std::min((int64_t)window + max_q - 1, max_len) : max_len;
 }
 
+fk_status check_plan(const char* fn, const fk_kv_cache* cache, int q_heads, int B, int max_q, int64_t max_len, int window, char* buf, size_t buf_bytes,
+                     KVView* c) {
+    if (!buf || buf_bytes == 0) {
+        set_error("%s: no buffer", fn);
+        return FK_EINVAL;
+    }
+    snprintf(buf, buf_bytes, "unsupported");
+    fk_status why;
+    if (!view_of(fn, cache, false, c, &why)) return why;
+    FK_TRY(check_queries(fn, *c, q_heads, 0, B, max_q, max_len));
+    if (max_len < 1 || window < 0) {
+        set_error("%s: max_len=%lld is not positive or window=%d is negative", fn, (long long)max_len, window);
+        return FK_EINVAL;
+    }
+    return FK_OK;
+}
+
+void describe_plan(const KVPlan& p, const KVView& c, int B, const char* more, char* buf, size_t buf_bytes) {
+    const size_t bytes = align_up(kv_partial_bytes(p, c.d, c.heads, B), 256) + 256;
+    if (p.join)
+        snprintf(buf, buf_bytes, "rows_shared(tiles=%d,row_blocks=%d,splits=%d,chunk=%lld%s) workspace=%zu", p.tiles, p.row_blocks, p.splits,
+                 (long long)(p.splits > 1 ? p.chunk : 0), more, bytes);
+    else
+        snprintf(buf, buf_bytes, "rows_own(tiles=%d,row_blocks=%d,waves=%d%s) workspace=%zu", p.tiles, p.row_blocks, own_waves(p.tiles),
+                 p.row_blocks < own_waves(p.tiles) ? ",packed" : "", bytes);
+}
+
 }  // namespace fk
 
 using namespace fk;
@@ -160,28 +187,9 @@ size_t fk_kv_workspace_bytes(const fk_kv_cache* cache, int q_heads, int64_t Tq, 
 }
 
 int fk_kv_plan(const fk_kv_cache* cache, int q_heads, int B, int max_q, int64_t max_len, int window, char* buf, size_t buf_bytes) {
-    const char* fn = "fk_kv_plan";
-    if (!buf || buf_bytes == 0) {
-        set_error("%s: no buffer", fn);
-        return FK_EINVAL;
-    }
-    snprintf(buf, buf_bytes, "unsupported");
     KVView c;
-    fk_status why;
-    if (!view_of(fn, cache, false, &c, &why)) return why;
-    FK_TRY(check_queries(fn, c, q_heads, 0, B, max_q, max_len));
-    if (max_len < 1 || window < 0) {
-        set_error("%s: max_len=%lld is not positive or window=%d is negative", fn, (long long)max_len, window);
-        return FK_EINVAL;
-    }
-    const KVPlan p = choose_kv_plan(c, q_heads, B, max_q, reach_of(window, max_q, max_len));
-    const size_t bytes = align_up(kv_partial_bytes(p, c.d, c.heads, B), 256) + 256;
-    if (p.join)
-        snprintf(buf, buf_bytes, "rows_shared(tiles=%d,row_blocks=%d,splits=%d,chunk=%lld) workspace=%zu", p.tiles, p.row_blocks, p.splits,
-                 (long long)(p.splits > 1 ? p.chunk : 0), bytes);
-    else
-        snprintf(buf, buf_bytes, "rows_own(tiles=%d,row_blocks=%d,waves=%d%s) workspace=%zu", p.tiles, p.row_blocks, own_waves(p.tiles),
-                 p.row_blocks < own_waves(p.tiles) ? ",packed" : "", bytes);
+    FK_TRY(check_plan("fk_kv_plan", cache, q_heads, B, max_q, max_len, window, buf, buf_bytes, &c));
+    describe_plan(choose_kv_plan(c, q_heads, B, max_q, reach_of(window, max_q, max_len)), c, B, "", buf, buf_bytes);
     return FK_OK;
 }
 

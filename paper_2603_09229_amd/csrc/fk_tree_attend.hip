@@ -48,9 +48,26 @@ static KVPlan choose_tree_plan(const KVView& c, int q_heads, int B, int max_q, i
     return p;
 }
 
+// Ragged sequences: the longest first, where there are rounds of workgroups and these are long enough for the look at the lengths.  8 trees of 121 tokens over
+// up to 20000 361 us in the order of the call, 346 so; 40 of 64 over up to 4096 (16 steps) 126 and 133.
+static bool comes_longest_first(const KVView& c, const KVPlan& p, int B, int64_t reach, int window) {
+    const int64_t blocks = (int64_t)B * c.heads * p.row_blocks, steps = cdiv(reach, (int64_t)kJoinWaves * kStep);
+    return p.join && p.splits == 1 && !window && B > 1 && B <= 64 && blocks > device_cu_count() && steps >= 32;
+}
+
 }  // namespace fk
 
 using namespace fk;
+
+extern "C" int fk_kv_plan_tree(const fk_kv_cache* cache, int q_heads, int B, int max_q, int64_t max_len, int window, char* buf, size_t buf_bytes) {
+    KVView c;
+    FK_TRY(check_plan("fk_kv_plan_tree", cache, q_heads, B, max_q, max_len, window, buf, buf_bytes, &c));
+    window = std::min(window, 1 << 30);
+    const int64_t reach = reach_of(window, max_q + 1, max_len);
+    const KVPlan p = choose_tree_plan(c, q_heads, B, max_q, reach);
+    describe_plan(p, c, B, comes_longest_first(c, p, B, reach, window) ? ",longest_first" : "", buf, buf_bytes);
+    return FK_OK;
+}
 
 extern "C" fk_status fk_kv_attend_tree(const fk_kv_cache* cache, const void* q, int64_t q_token_stride, int64_t q_head_stride, int q_heads,
                                        int64_t Tq, const int32_t* pages, int max_pages, const int32_t* lens, const int32_t* q_start, int B,
@@ -90,7 +107,8 @@ extern "C" fk_status fk_kv_attend_tree(const fk_kv_cache* cache, const void* q, 
     FK_TRY(need(fn, "out", out, 16));
     if (lse) FK_TRY(need(fn, "lse", lse, 4));
     FK_TRY(need(fn, "ws", ws, 256));
-    const KVPlan p = choose_tree_plan(c, q_heads, B, max_q, reach_of(window, max_q + 1, max_len));
+    const int64_t reach = reach_of(window, max_q + 1, max_len);
+    const KVPlan p = choose_tree_plan(c, q_heads, B, max_q, reach);
     const size_t bytes = kv_partial_bytes(p, c.d, c.heads, B);
     if (ws_bytes < bytes) {
         set_error("%s: workspace too small: %zu bytes given, %zu needed", fn, ws_bytes, bytes);
@@ -98,9 +116,5 @@ extern "C" fk_status fk_kv_attend_tree(const fk_kv_cache* cache, const void* q, 
     }
     const KVAttend a{{(const uint16_t*)q, q_token_stride, q_head_stride}, q_heads, Tq, pages, lens, q_start, max_pages, B, max_q,
                      scale, 0, window, (uint16_t*)out, lse, (float*)ws, tree, words};
-    const int64_t blocks = (int64_t)B * c.heads * p.row_blocks, steps = cdiv(reach_of(window, max_q + 1, max_len), (int64_t)kJoinWaves * kStep);
-    // Ragged sequences: the longest first, where there are rounds of workgroups and these are long enough for the look at the lengths.  8 trees of 121 tokens over
-    // up to 20000 361 us in the order of the call, 346 so; 40 of 64 over up to 4096 (16 steps) 126 and 133.
-    const bool longest_first = p.join && p.splits == 1 && !window && B > 1 && B <= 64 && blocks > device_cu_count() && steps >= 32;
-    return launch_attend<true>(c, a, p, (hipStream_t)stream, longest_first);
+    return launch_attend<true>(c, a, p, (hipStream_t)stream, comes_longest_first(c, p, B, reach, window));
 }
