@@ -440,8 +440,9 @@ size_t fk_kv_choose_workspace_bytes(const fk_kv_cache* cache, int B, int64_t max
  *   kept       device, [B, kept_heads, max_kept] int32; kept_heads 1 (the same places for all heads) or cache->heads
  *   counts     device, [B] int32 (at most max_kept count)
  *   start      device, [B] int32, or NULL: 0
- *   to_pages   device, [B, to_max_pages] int32: where the rows go, or NULL or `pages`: in place.  In place kept[b, h] ascends (no place twice), so
- *              that no row moves back; other pages have none in common with those that are read.  No page is written for two sequences.
+ *   to_pages   device, [B, to_max_pages] int32: where the rows go, or NULL or `pages`: in place.  In place kept[b, h] ascends (no place twice) with
+ *              kept[b, h, j] >= j, but for places that are left out, so that no row moves back; other pages have none in common with those that
+ *              are read.  No page is written for two sequences.
  *   mass       device, [pages, heads, page_size] float, or NULL: weights that move with their rows
  * Cutting down to the places of fk_kv_choose has start = NULL; an accepted branch of a drafted tree has the number of tokens before the tree in
  * start and the branch's tokens, counted within the tree, in kept.  The sequence's length is then start + counts.  A row whose place is

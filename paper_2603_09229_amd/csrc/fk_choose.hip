@@ -8,10 +8,13 @@
 // A workgroup holds the weights of a sequence and head in registers, read once.  Sequences of more than kWhole tokens are divided among
 // workgroups, and the four steps are launches of their own: each counts its part, the next one adds the parts' counts up.
 //
-// What bounds it: latency, of the page and the weight behind each other, of three rounds of counting with three barriers each, and of the
-// places' prefix sums.  8 heads: one sequence of 1100 tokens 6.5 us, 64 of up to 8192 13.6 (15 MB, 1.1 TB/s; counted one weight a thread at a time from memory
-// 29), one of 131072 in 16 parts 23.8 (in one workgroup 299).  Counts are held four times: weights are bell-shaped or worse, and lanes with the
-// same leading bits wait for each other.  Sums within a wave go by DPP, six instructions instead of six trips through LDS.
+// What bounds it.  One short sequence: latency, of the page and the weight behind each other, of three rounds of counting with three barriers each, and
+// of the places' prefix sums.  A batch: about 550 vector instructions a wave, issued in 58 % of the cycles, and additions in LDS that meet in a
+// bank, 46 % of its time: the leading 11 bits are sign, exponent and two bits of mantissa, and most weights fall into few of them.  In parts: four
+// launches behind each other, and in the last three every workgroup adds all parts' counts up for the bin that all of them find.  8 heads: one sequence of 1100
+// tokens 6.5 us, 64 of up to 8192 13.9 (15 MB, 1.1 TB/s; counted one weight a thread at a time from memory 29), one of 131072 in 16 parts 23.8 (in
+// one workgroup 299).  Counts are held four times, so that lanes with the same leading bits wait less for each other.  Sums within a wave go by DPP,
+// six instructions instead of six trips through LDS.
 #include <algorithm>
 
 #include "fk_device.h"
@@ -20,8 +23,8 @@
 namespace fk {
 
 constexpr int kChooseThreads = 1024, kChooseWaves = kChooseThreads / 64;
-// Most tokens that one workgroup holds in registers.  8 heads of one sequence: 9000 tokens 13.7 us; 32 a thread no longer fit, 32000 tokens 54, and 33000 in
-// parts 22.
+// Most tokens that one workgroup holds in registers.  8 heads of one sequence: 9000 tokens 13.7 us (five of 16 a thread's registers go through scratch
+// memory: the bound of 64 lets workgroups run in pairs); 32 a thread no longer fit, 32000 tokens 54, and 33000 in parts 22.
 constexpr int kWhole = 16 * kChooseThreads;
 constexpr int kPart = 8 * kChooseThreads;     // fewest of a part
 constexpr int kMostParts = 64;

@@ -371,7 +371,7 @@ __device__ __forceinline__ float lse_of(float top, float sum) {
     return sum > 0.f || sum != sum ? (top + __log2f(sum)) * 0.6931471805599453f : -INFINITY;
 }
 
-// The sequence that is longer than `rank` others (of equal ones the later), of up to 64.
+// The sequence that `rank` others come before, of up to 64: the longer ones, and of equal ones those before it.
 __device__ __forceinline__ int of_rank(const int32_t* lens, int B, int rank, int lane) {
     const int mine = lane < B ? lens[lane] : INT32_MIN;
     int longer = lane < B ? 0 : B;
@@ -525,7 +525,8 @@ struct Softmax {
 // further); otherwise each wave has rows of its own, of one sequence or, where that has fewer tiles than a workgroup has waves, of
 // several, and takes all steps that they see.  Codes go straight from the cache into operands.
 // Two tiles of trees of 64 channels are held to 128 registers, so that workgroups run in pairs on a compute unit: 12 trees of 100 tokens over 5000
-// 124 us, where three tiles take 137 and four 132.
+// 124 us, where three tiles take 137 and four 132.  For that 11 registers (bf16) or 17 (fp16) go through scratch memory, 48 and 56 bytes a lane;
+// elsewhere it is one, at three tiles of 128 channels.
 template <bool BF, int ND, int NT, bool JOIN, bool TREE>
 __global__ __launch_bounds__(64 * (JOIN ? kJoinWaves : own_waves(NT)), NT == 1 && ND <= 4 ? 4 : JOIN ? (TREE && NT == 2 && ND == 2 ? 4 : 1) : 2)
 void kv_attend_kernel(AttendArgs A) {

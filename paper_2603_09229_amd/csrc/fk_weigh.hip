@@ -11,9 +11,11 @@
 // adds their parts in order: no atomics, and no result depends on the order of workgroups.
 //
 // Two forms.  Few rows (up to 128 at 128 channels) stay in LDS, and waves go over the tokens with the next step's codes on their way; the
-// workgroup's four waves a SIMD hide the rest.  Bound by bytes: 64 sequences of up to 8192 tokens, 8 heads of 128, 198 MB in 51 us, 3.9 TB/s
-// (one of 700: 4.4 us).  More rows stream by in blocks of two buffers, rows that all see all tokens with the products of a tile under
-// the exponentials of the one before it: 2 x 4096 queries of 32 heads over up to 9000 tokens, 426 GFLOP in 482 us, 0.88 PFLOP/s.
+// workgroup's four waves a SIMD hide the rest.  Bound by bytes: 64 sequences of up to 8192 tokens, 8 heads of 128, 198 MB in 52 us, 3.8 TB/s
+// (one of 700: 4.8 us).  A tile's read, products and exponentials follow each other there, so that with some dozen rows they bound it instead: 6 x 32
+// queries of 64 channels over up to 15000 tokens 17 us, where bytes take 4.  More rows stream by in blocks of two buffers, rows that all see all tokens with the products of a tile under
+// the exponentials of the one before it: 2 x 4096 queries of 32 heads over up to 9000 tokens, 426 GFLOP in 481 us, 0.89 PFLOP/s
+// (256 channels: three registers go through scratch memory).
 // A tile of 16 rows and 64 tokens at d = 128 is 16 MFMA (256 cycles) and 16 times multiply-add, exponential and addition (another 256); alone
 // in a loop the two overlap to 412, here they take about 500: the rest is what a wave needs between tiles and at the blocks' barriers.
 // (The simple form, tokens on the tiles' row side and each wave reading the queries from memory: 1019 us.  Keys of 32 tokens and four waves a SIMD spill:
@@ -50,7 +52,8 @@ struct WeighArgs {
 // LDS: the table of pairs of the keys' levels, 256 rows of 32 copies, in the lower halves of rows of 256 bytes (a byte of codes is then the
 // address with one v_perm), and the queries in the upper ones, in the order in which a wave's lanes read them as operands, 16 bytes a lane.
 // Lanes that write a row's pieces meet in a bank unless the rows' order within a piece's slot is turned by the piece, and by no more of the quarter
-// than its upper bit, or lanes of two quarters meet when they read (conflicts 39 % of the LDS's time, so 13 %).
+// than its upper bit, or lanes of two quarters meet when they read (conflicts 39 % of the LDS's time, so 13 %, which the
+// cycles do not show: the LDS is busy for a fifth of them).
 template <bool STREAM>
 struct WeighLds {
     static constexpr int bytes = 65536 * (STREAM ? 2 : 1), piece_bytes = STREAM ? 1024 : 2048;

@@ -77,8 +77,8 @@ def tree_masks(parents: list[list[int]], device=None) -> tuple[torch.Tensor, lis
 class Server:
     """A batch of sequences over one cache: slots are given out page by page, prompts and steps go through the three calls.
 
-    max_len: tokens that a sequence holds at a time; max_pos: tokens that it may have in all, where some are evicted (max_len if not given);
-    weights: every step adds its attention weights up, so that `evict` knows what to keep."""
+    max_len: tokens that a sequence holds at a time; max_pos: positions that it may take in all, where some tokens are evicted (max_len if not
+    given: an eviction then frees places, but no positions); weights: every step adds its attention weights up, so that `evict` knows what to keep."""
 
     max_pos = None
     mass = None                                                       # attention weights of the cached tokens, with `weights`
