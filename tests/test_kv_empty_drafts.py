@@ -1,4 +1,4 @@
-"""kv_cache.Server where no sequence has a tree this time: `draft` and `accept` as in any other round of a program's loop.  No kernel is launched
+"""kv_cache.Server where no sequence has a tree this time: `draft` and `accept` as in any other pass of a loop.  No kernel is launched
 here."""
 import pytest
 import torch
@@ -23,7 +23,7 @@ def test_a_draft_for_no_one_is_accepted():
 def test_nothing_waits_for_an_accept_that_has_nothing_to_do():
     s = server([5, 20])
     s.draft(*rows(0, 0, 0), [[], []])
-    assert s.step(*rows(0, 0, 0), [0, 0]).shape == (0, 2, 32)     # not held up, and the round is over
+    assert s.step(*rows(0, 0, 0), [0, 0]).shape == (0, 2, 32)     # not held up, and the draft is over
     with pytest.raises(ValueError, match="no draft"):
         s.accept([[], []])
     s.draft(*rows(0, 0, 0), [[], []])
